@@ -1,0 +1,285 @@
+// C ABI of the paged 4-bit cache (see include/mars_cache.h): argument checks, workspace carving and kernel launches.  Nothing
+// here allocates or synchronises.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/mars_cache.h"
+#include "kv_attention.h"
+#include "kv_format.h"
+#include "kv_pages.h"
+#include "kv_rows.h"
+
+namespace mars {
+namespace kv {
+
+constexpr size_t kAlign = 256;
+static size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+static int launched() { return hipGetLastError() == hipSuccess ? MARS_OK : MARS_ERR_HIP; }
+
+enum { POOL = 1, TABLE = 2, LENS = 4, HELD = 8, REFS = 16 };
+
+// The cache as the kernels see it, if it is one and has the tables that a call names.
+static bool cache_ok(const mars_kv_cache* k, int needs, Cache* c) {
+  if (!k || k->layers < 1 || k->pages < 1 || k->heads < 1 || k->sequences < 1 || k->width < 1) return false;
+  if (mars_kv_head_bytes(k->dim, k->page) == 0) return false;
+  if (((needs & POOL) && !k->pool) || ((needs & TABLE) && !k->page_table) || ((needs & LENS) && !k->lens) ||
+      ((needs & HELD) && !k->held) || ((needs & REFS) && !k->refs))
+    return false;
+  if (reinterpret_cast<uintptr_t>(k->pool) % 16) return false;
+  int log_page = 3;
+  while ((1 << log_page) < k->page) ++log_page;
+  const size_t blk = head_bytes(k->dim, k->page), page_bytes = blk * k->heads;
+  if (page_bytes > (1u << 30) || k->pages > (1 << 30) || static_cast<long>(k->width) * k->page > (1l << 30)) return false;
+  *c = Cache{static_cast<uint8_t*>(k->pool), k->page_table, k->lens, k->held, k->refs, page_bytes * k->pages,
+             static_cast<u32>(page_bytes), static_cast<u32>(blk), k->layers, k->pages, k->heads, log_page, k->sequences, k->width};
+  return true;
+}
+static bool batch_ok(int B, int N) { return B >= 1 && B <= MARS_KV_MAX_REQUESTS && N >= 1 && N <= (1 << 24); }
+static bool dtype_ok(int dtype) { return dtype == MARS_F32 || dtype == MARS_BF16; }
+static bool rows_ok(const mars_kv_rows* r, int dtype) {
+  if (!r || !r->data || reinterpret_cast<uintptr_t>(r->data) % 16) return false;
+  const int64_t step = dtype == MARS_F32 ? 4 : 8;
+  return r->request % step == 0 && r->node % step == 0 && r->head % step == 0;
+}
+template <typename T> static Rows<T> rows_of(const mars_kv_rows* r) { return Rows<T>{static_cast<T*>(r->data), r->request, r->node, r->head}; }
+
+// f(integral_constant<dim>).
+template <typename F> static int by_dim(int dim, F f) {
+  switch (dim) {
+    case 64: return f(std::integral_constant<int, 64>{});
+    case 128: return f(std::integral_constant<int, 128>{});
+    default: return f(std::integral_constant<int, 256>{});
+  }
+}
+// f(a value of the element type).
+template <typename F> static int by_type(int dtype, F f) { return dtype == MARS_F32 ? f(float{}) : f(bf16_t{}); }
+
+static int row_octets(int N) { return (N + 6) / 8 + 1; }  // octets that N positions can touch
+
+// ---------------------------------------------------------------- attention: how the work is laid out
+struct AttnPlan {
+  int mode, blocks_rb;  // waves divide keys or rows; blocks of 16 rows per wave
+  u32 groups, least;    // work-groups; least units each takes
+  size_t bytes;         // of pieces
+};
+static size_t piece_bytes(int dim, int rb) { return sizeof(float) * (32 * rb + static_cast<size_t>(rb) * (dim / 16) * 256); }
+
+static AttnPlan attn_plan(int B, int N, int group, int dim, int dtype) {
+  (void)B;
+  const long rows = static_cast<long>(N) * group;
+  AttnPlan p;
+  p.mode = KEYS;
+  if (dtype == MARS_F32) {
+    p.blocks_rb = 1;
+    if (rows > 16) p.mode = ROWS;
+  } else if (rows <= 16) {
+    p.blocks_rb = 1;
+  } else if (rows <= 32 || (dim == 256 && rows <= 64)) {
+    p.blocks_rb = 2;
+  } else {
+    p.blocks_rb = dim == 256 ? 2 : 4;
+    if (rows > 64) p.mode = ROWS;
+  }
+  p.groups = p.blocks_rb == 1 ? 1024 : p.blocks_rb == 2 ? 512 : 256;
+  p.least = 1;
+  p.bytes = align_up(static_cast<size_t>(p.groups) * 2 * (p.mode == ROWS ? 4 : 1) * piece_bytes(dim, p.blocks_rb));
+  return p;
+}
+
+template <int D, int RB, typename T, int MODE> static int launch_attention(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE>), dim3(p.groups), dim3(kThreads), 0, stream, a, p.least);
+  if (hipGetLastError() != hipSuccess) return MARS_ERR_HIP;
+  hipLaunchKernelGGL((merge_kernel<D, RB, T, MODE>), dim3(p.groups - 1, MODE == ROWS ? RB : 1), dim3(kThreads), 0, stream, a, p.groups, p.least);
+  return launched();
+}
+
+static ReserveSpace reserve_space(char* ws, int pages, int B) {
+  ReserveSpace r;
+  const size_t n = align_up(sizeof(int32_t) * B);
+  r.shared = reinterpret_cast<int32_t*>(ws);
+  r.wants = reinterpret_cast<int32_t*>(ws + n);
+  r.begin = reinterpret_cast<int32_t*>(ws + 2 * n);
+  r.copy_src = reinterpret_cast<int32_t*>(ws + 3 * n);
+  r.copy_dst = reinterpret_cast<int32_t*>(ws + 4 * n);
+  r.copies = reinterpret_cast<int32_t*>(ws + 5 * n);
+  r.found = reinterpret_cast<int32_t*>(ws + 5 * n + kAlign);
+  (void)pages;
+  return r;
+}
+static u32 copy_groups(const Cache& c, long pairs) {
+  const long items = pairs * c.layers * ((c.page_bytes + kCopyPart - 1) / kCopyPart);
+  return static_cast<u32>(items < 2048 ? items : 2048);
+}
+
+}  // namespace kv
+}  // namespace mars
+
+using namespace mars::kv;
+
+extern "C" {
+
+size_t mars_kv_head_bytes(int dim, int page) {
+  if ((dim != 64 && dim != 128 && dim != 256) || page < 8 || page > 256 || (page & (page - 1))) return 0;
+  return head_bytes(dim, page);
+}
+
+int mars_kv_append(const mars_kv_cache* cache, int layer, const int32_t* seqs, const mars_kv_rows* k, const mars_kv_rows* v,
+                   int dtype, const int32_t* n_new, int B, int N, int32_t* status, void* hip_stream) {
+  Cache c;
+  if (!batch_ok(B, N) || !cache_ok(cache, POOL | TABLE | LENS, &c) || layer < 0 || layer >= c.layers) return MARS_ERR_ARG;
+  if (!dtype_ok(dtype)) return MARS_ERR_DTYPE;
+  if (!rows_ok(k, dtype) || !rows_ok(v, dtype)) return MARS_ERR_ARG;
+  const int octets = row_octets(N), per_group = 2048 / cache->dim;
+  const long items = static_cast<long>(B) * octets * c.heads, groups = (items + per_group - 1) / per_group;
+  if (groups > 0x7FFFFFFFl) return MARS_ERR_ARG;
+  return by_dim(cache->dim, [&](auto dim) {
+    return by_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      hipLaunchKernelGGL((append_kernel<decltype(dim)::value, T>), dim3(static_cast<u32>(groups)), dim3(256), 0, static_cast<hipStream_t>(hip_stream), c,
+                         c.layer_bytes * layer, seqs, rows_of<const T>(k), rows_of<const T>(v), n_new, B, N, octets, items, status);
+      return launched();
+    });
+  });
+}
+
+int mars_kv_read(const mars_kv_cache* cache, int layer, const int32_t* seqs, const int32_t* first, const mars_kv_rows* k,
+                 const mars_kv_rows* v, int dtype, int B, int N, void* hip_stream) {
+  Cache c;
+  if (!batch_ok(B, N) || !cache_ok(cache, POOL | TABLE, &c) || layer < 0 || layer >= c.layers) return MARS_ERR_ARG;
+  if (!dtype_ok(dtype)) return MARS_ERR_DTYPE;
+  if (!rows_ok(k, dtype) || !rows_ok(v, dtype)) return MARS_ERR_ARG;
+  const int octets = row_octets(N), per_group = 2048 / cache->dim;
+  const long items = static_cast<long>(B) * octets * c.heads, groups = (items + per_group - 1) / per_group;
+  if (groups > 0x7FFFFFFFl) return MARS_ERR_ARG;
+  return by_dim(cache->dim, [&](auto dim) {
+    return by_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      hipLaunchKernelGGL((read_kernel<decltype(dim)::value, T>), dim3(static_cast<u32>(groups)), dim3(256), 0, static_cast<hipStream_t>(hip_stream), c,
+                         c.layer_bytes * layer, seqs, first, rows_of<T>(k), rows_of<T>(v), B, N, octets, items);
+      return launched();
+    });
+  });
+}
+
+int mars_tree_mask(const int32_t* tree_parent, const int32_t* n_new, int B, int N, uint64_t* mask, int32_t* status, void* hip_stream) {
+  if (!tree_parent || !mask || B < 1 || B > MARS_KV_MAX_REQUESTS || N < 1 || N > MARS_MAX_NODES) return MARS_ERR_ARG;
+  hipLaunchKernelGGL(tree_mask_kernel, dim3(B), dim3(kMaskThreads), 0, static_cast<hipStream_t>(hip_stream), tree_parent, n_new, N,
+                     reinterpret_cast<unsigned long long*>(mask), status);
+  return launched();
+}
+
+static bool attention_sizes_ok(int B, int N, int q_heads, int heads, int dim) {
+  return batch_ok(B, N) && heads >= 1 && q_heads >= heads && q_heads % heads == 0 && q_heads <= (1 << 16) && mars_kv_head_bytes(dim, 8) != 0 &&
+         static_cast<long>(N) * (q_heads / heads) <= (1l << 28);
+}
+
+size_t mars_kv_attention_workspace_bytes(int B, int N, int q_heads, int heads, int dim, int dtype) {
+  if (!attention_sizes_ok(B, N, q_heads, heads, dim) || !dtype_ok(dtype)) return 0;
+  return attn_plan(B, N, q_heads / heads, dim, dtype).bytes;
+}
+
+int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs, const mars_kv_rows* q, int dtype, int q_heads,
+                      const int32_t* n_new, const uint64_t* mask, float scale, int max_len, const mars_kv_rows* out, float* lse,
+                      int B, int N, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  Cache c;
+  if (!batch_ok(B, N) || !cache_ok(cache, POOL | TABLE | LENS, &c) || layer < 0 || layer >= c.layers ||
+      !attention_sizes_ok(B, N, q_heads, c.heads, cache->dim))
+    return MARS_ERR_ARG;
+  if (!dtype_ok(dtype)) return MARS_ERR_DTYPE;
+  if (!rows_ok(q, dtype) || !rows_ok(out, dtype) || max_len < 0 || !(scale > 0.0f) || !std::isfinite(scale) || (mask && N > MARS_MAX_NODES))
+    return MARS_ERR_ARG;
+  const AttnPlan p = attn_plan(B, N, q_heads / c.heads, cache->dim, dtype);
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < p.bytes) return MARS_ERR_WORKSPACE;
+  AttnArgs a{};
+  a.c = c;
+  a.layer_offset = c.layer_bytes * layer;
+  a.seqs = seqs;
+  a.n_new = n_new;
+  a.mask = reinterpret_cast<const unsigned long long*>(mask);
+  a.q = q->data;
+  a.q_request = q->request; a.q_node = q->node; a.q_head = q->head;
+  a.out = out->data;
+  a.out_request = out->request; a.out_node = out->node; a.out_head = out->head;
+  a.lse = lse;
+  a.partial = static_cast<float*>(workspace);
+  a.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
+  a.B = B; a.N = N; a.q_heads = q_heads; a.group = q_heads / c.heads; a.words = (N + 63) / 64;
+  // the deal counts units in 32 bits
+  const int rows_item = (p.mode == ROWS ? 64 : 16) * p.blocks_rb, unit = p.mode == ROWS ? kTile : 4 * kTile;
+  const double units = static_cast<double>(B) * c.heads * ((static_cast<long>(N) * a.group + rows_item - 1) / rows_item) *
+                       (((static_cast<long>(c.width) << c.log_page) + N + unit - 1) / unit);
+  if (units > 4.0e9) return MARS_ERR_ARG;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  return by_dim(cache->dim, [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    if (dtype == MARS_F32) return p.mode == KEYS ? launch_attention<D, 1, float, KEYS>(p, a, stream) : launch_attention<D, 1, float, ROWS>(p, a, stream);
+    if (p.mode == KEYS) {
+      if (p.blocks_rb == 1) return launch_attention<D, 1, bf16_t, KEYS>(p, a, stream);
+      if (p.blocks_rb == 2) return launch_attention<D, 2, bf16_t, KEYS>(p, a, stream);
+    }
+    if constexpr (D == 256) return launch_attention<D, 2, bf16_t, ROWS>(p, a, stream);
+    else return p.mode == KEYS ? launch_attention<D, 4, bf16_t, KEYS>(p, a, stream) : launch_attention<D, 4, bf16_t, ROWS>(p, a, stream);
+  });
+}
+
+int mars_kv_commit(const mars_kv_cache* cache, const int32_t* seqs, const int32_t* accept_len, const int32_t* path_idx, int B, int N,
+                   int32_t* new_lens, int32_t* status, void* hip_stream) {
+  Cache c;
+  if (!batch_ok(B, N) || !cache_ok(cache, POOL | TABLE | LENS, &c) || !accept_len || !path_idx || !new_lens) return MARS_ERR_ARG;
+  const long groups = static_cast<long>(B) * c.layers * ((c.heads + 3) / 4);
+  if (groups > 0x7FFFFFFFl) return MARS_ERR_ARG;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  int32_t* apart = new_lens == c.lens ? nullptr : new_lens;
+  const int rc = by_dim(cache->dim, [&](auto dim) {
+    hipLaunchKernelGGL((commit_kernel<decltype(dim)::value>), dim3(static_cast<u32>(groups)), dim3(256), 0, stream, c, seqs, accept_len, path_idx, B, N,
+                       apart, status);
+    return launched();
+  });
+  if (rc != MARS_OK || apart) return rc;
+  hipLaunchKernelGGL(commit_lens_kernel, dim3((B + 3) / 4), dim3(256), 0, stream, c, seqs, accept_len, path_idx, B, N);
+  return launched();
+}
+
+size_t mars_kv_reserve_workspace_bytes(int pages, int B) {
+  if (pages < 1 || pages > (1 << 30) || B < 1 || B > MARS_KV_MAX_REQUESTS) return 0;
+  return 5 * align_up(sizeof(int32_t) * B) + kAlign + align_up(sizeof(int32_t) * pages);
+}
+
+int mars_kv_reserve(const mars_kv_cache* cache, const int32_t* seqs, const int32_t* n_new, int B, int N, int32_t* status, void* workspace,
+                    size_t workspace_bytes, void* hip_stream) {
+  Cache c;
+  if (!batch_ok(B, N) || !cache_ok(cache, POOL | TABLE | LENS | HELD | REFS, &c)) return MARS_ERR_ARG;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < mars_kv_reserve_workspace_bytes(c.pages, B))
+    return MARS_ERR_WORKSPACE;
+  const ReserveSpace ws = reserve_space(static_cast<char*>(workspace), c.pages, B);
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kPlanThreads), 0, stream, c, seqs, n_new, B, N, status, ws);
+  if (hipGetLastError() != hipSuccess) return MARS_ERR_HIP;
+  hipLaunchKernelGGL(copy_pages_kernel, dim3(copy_groups(c, B)), dim3(256), 0, stream, c, ws.copy_src, ws.copy_dst, ws.copies, 0);
+  return launched();
+}
+
+int mars_kv_fork(const mars_kv_cache* cache, const int32_t* src, const int32_t* dst, int B, int32_t* status, void* hip_stream) {
+  Cache c;
+  if (!batch_ok(B, 1) || !cache_ok(cache, TABLE | LENS | HELD | REFS, &c) || !src || !dst) return MARS_ERR_ARG;
+  hipLaunchKernelGGL(fork_kernel, dim3(B), dim3(256), 0, static_cast<hipStream_t>(hip_stream), c, src, dst, status);
+  return launched();
+}
+
+int mars_kv_release(const mars_kv_cache* cache, const int32_t* seqs, int B, int32_t* status, void* hip_stream) {
+  Cache c;
+  if (!batch_ok(B, 1) || !cache_ok(cache, TABLE | LENS | HELD | REFS, &c)) return MARS_ERR_ARG;
+  hipLaunchKernelGGL(release_kernel, dim3(B), dim3(256), 0, static_cast<hipStream_t>(hip_stream), c, seqs, status);
+  return launched();
+}
+
+int mars_kv_copy_pages(const mars_kv_cache* cache, const int32_t* src, const int32_t* dst, int n, void* hip_stream) {
+  Cache c;
+  if (n < 1 || !cache_ok(cache, POOL, &c) || !src || !dst) return MARS_ERR_ARG;
+  hipLaunchKernelGGL(copy_pages_kernel, dim3(copy_groups(c, n)), dim3(256), 0, static_cast<hipStream_t>(hip_stream), c, src, dst, nullptr, n);
+  return launched();
+}
+
+}  // extern "C"
