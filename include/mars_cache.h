@@ -108,7 +108,7 @@ int mars_tree_mask(const int32_t* tree_parent, const int32_t* n_new, int B, int 
  * Attention of N query rows per request (the nodes that mars_kv_append put behind the committed tokens) over the cache:
  *   out[b][i][h] = sum_j p_j v_j,  p = softmax_j(scale * q[b][i][h] . k_j),  keys and values of cache head h / (q_heads / heads),
  * over the committed tokens j < lens[s] and the nodes that row i sees.  A row that sees nothing gets zeros.
- *   q, out     rows [B][N][q_heads][dim] of `dtype` (MARS_F32 or MARS_BF16); q_heads a multiple of heads.
+ *   q, out     rows [B][N][q_heads][dim] of `dtype` (MARS_F32 or MARS_BF16); q_heads a multiple of heads, at most 64 times it.
  *   lse        out, optional, [B][N][q_heads] fp32: log sum_j exp(scale * q.k_j); -inf for a row that sees nothing.
  *   n_new      [B], or NULL: N for all.  Rows from n_new[b] on see nothing, not even committed tokens.
  *   mask       [B][N][(N + 63)/64] uint64, bit j of row i: row i sees node j (any mask; mars_tree_mask makes a tree's); N <= MARS_MAX_NODES.

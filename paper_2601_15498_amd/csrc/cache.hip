@@ -61,6 +61,7 @@ static int row_octets(int N) { return (N + 6) / 8 + 1; }  // octets that N posit
 // ---------------------------------------------------------------- attention: how the work is laid out
 struct AttnPlan {
   int mode, blocks_rb;  // waves divide keys or rows; blocks of 16 rows per wave
+  int nodes;            // of a block of rows
   u32 groups, least;    // work-groups; least units each takes
   size_t bytes;         // of pieces
 };
@@ -76,22 +77,24 @@ static AttnPlan attn_plan(int B, int N, int group, int dim, int dtype) {
     if (rows > 16) p.mode = ROWS;
   } else if (rows <= 16) {
     p.blocks_rb = 1;
-  } else if (rows <= 32 || (dim == 256 && rows <= 64)) {
+  } else if (rows <= 32) {
     p.blocks_rb = 2;
   } else {
-    p.blocks_rb = dim == 256 ? 2 : 4;
-    if (rows > 64) p.mode = ROWS;
+    p.blocks_rb = 2;
+    p.mode = ROWS;
   }
-  p.groups = p.blocks_rb == 1 ? 1024 : p.blocks_rb == 2 ? 512 : 256;
+  p.groups = p.blocks_rb == 1 ? 1024 : 512;
   p.least = 1;
+  p.nodes = (p.mode == ROWS ? 64 : 16) * p.blocks_rb / group;
   p.bytes = align_up(static_cast<size_t>(p.groups) * 2 * (p.mode == ROWS ? 4 : 1) * piece_bytes(dim, p.blocks_rb));
   return p;
 }
 
 template <int D, int RB, typename T, int MODE> static int launch_attention(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE>), dim3(p.groups), dim3(kThreads), 0, stream, a, p.least);
+  if (a.c.log_page >= 5) hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE, true>), dim3(p.groups), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE, false>), dim3(p.groups), dim3(kThreads), 0, stream, a);
   if (hipGetLastError() != hipSuccess) return MARS_ERR_HIP;
-  hipLaunchKernelGGL((merge_kernel<D, RB, T, MODE>), dim3(p.groups - 1, MODE == ROWS ? RB : 1), dim3(kThreads), 0, stream, a, p.groups, p.least);
+  hipLaunchKernelGGL((merge_kernel<D, RB, T, MODE>), dim3(p.groups - 1, MODE == ROWS ? RB : 1), dim3(kThreads), 0, stream, a, p.groups);
   return launched();
 }
 
@@ -172,7 +175,7 @@ int mars_tree_mask(const int32_t* tree_parent, const int32_t* n_new, int B, int 
 
 static bool attention_sizes_ok(int B, int N, int q_heads, int heads, int dim) {
   return batch_ok(B, N) && heads >= 1 && q_heads >= heads && q_heads % heads == 0 && q_heads <= (1 << 16) && mars_kv_head_bytes(dim, 8) != 0 &&
-         static_cast<long>(N) * (q_heads / heads) <= (1l << 28);
+         q_heads / heads <= 64 && static_cast<long>(N) * (q_heads / heads) <= (1l << 28);
 }
 
 size_t mars_kv_attention_workspace_bytes(int B, int N, int q_heads, int heads, int dim, int dtype) {
@@ -206,21 +209,17 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
   a.partial = static_cast<float*>(workspace);
   a.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
   a.B = B; a.N = N; a.q_heads = q_heads; a.group = q_heads / c.heads; a.words = (N + 63) / 64;
+  a.nodes = p.nodes;
+  a.least = p.least;
   // the deal counts units in 32 bits
-  const int rows_item = (p.mode == ROWS ? 64 : 16) * p.blocks_rb, unit = p.mode == ROWS ? kTile : 4 * kTile;
-  const double units = static_cast<double>(B) * c.heads * ((static_cast<long>(N) * a.group + rows_item - 1) / rows_item) *
-                       (((static_cast<long>(c.width) << c.log_page) + N + unit - 1) / unit);
+  const double units = static_cast<double>(B) * c.heads * ((N + p.nodes - 1) / p.nodes) * (((static_cast<long>(c.width) << c.log_page) + N + 3 * kUnit) / kUnit);
   if (units > 4.0e9) return MARS_ERR_ARG;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   return by_dim(cache->dim, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
     if (dtype == MARS_F32) return p.mode == KEYS ? launch_attention<D, 1, float, KEYS>(p, a, stream) : launch_attention<D, 1, float, ROWS>(p, a, stream);
-    if (p.mode == KEYS) {
-      if (p.blocks_rb == 1) return launch_attention<D, 1, bf16_t, KEYS>(p, a, stream);
-      if (p.blocks_rb == 2) return launch_attention<D, 2, bf16_t, KEYS>(p, a, stream);
-    }
-    if constexpr (D == 256) return launch_attention<D, 2, bf16_t, ROWS>(p, a, stream);
-    else return p.mode == KEYS ? launch_attention<D, 4, bf16_t, KEYS>(p, a, stream) : launch_attention<D, 4, bf16_t, ROWS>(p, a, stream);
+    if (p.mode == ROWS) return launch_attention<D, 2, bf16_t, ROWS>(p, a, stream);
+    return p.blocks_rb == 1 ? launch_attention<D, 1, bf16_t, KEYS>(p, a, stream) : launch_attention<D, 2, bf16_t, KEYS>(p, a, stream);
   });
 }
 

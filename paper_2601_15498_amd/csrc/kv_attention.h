@@ -29,7 +29,9 @@ namespace mars {
 namespace kv {
 
 constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
 constexpr int kTile = 32;             // keys per wave and step
+constexpr int kUnit = kWaves * kTile; // keys of a unit of work: each wave fetches a tile of it
 constexpr float kFloor = -3.0e38f;    // the reference before the first key that counts
 constexpr float kSlack = 8.0f;        // how far (in powers of two) scores may pass the reference before it is moved up
 
@@ -47,6 +49,8 @@ struct AttnArgs {
   float* partial;
   float scale_log2;
   int B, N, q_heads, group, words;
+  int nodes;    // of a block of rows
+  u32 least;    // units a work-group takes at least
 };
 
 __device__ __forceinline__ float max3(float a, float b, float c) {  // (written out: fmaxf would first quiet each operand)
@@ -79,70 +83,295 @@ template <int TERMS> __device__ __forceinline__ void split_pair(float a, float b
   }
 }
 
-// The deal.  Request b has items[b] = heads x blocks of rows, each of tiles[b] units; units in front of it: begin.
-template <int ROWS_PER_ITEM, int UNIT> struct Deal {
-  int n, len, items, tiles;
-  __device__ __forceinline__ Deal(const AttnArgs& a, int b) {
+// ---------------------------------------------------------------- the deal
+// A request's items are (cache head, block of `nodes` nodes), its units those of its items.  Under a mask a block has all the request's keys.
+// In a chain it has those up to its last node, and blocks are taken in pairs, the last with the first and so on, so that every pair has about
+// the same number of units: `per`, which is rounded up (what is left over of it is idle).
+struct Request {
+  int n, len, blocks, pairs;  // pairs: of blocks, or blocks
+  u32 per;                    // units of a pair, or of a block
+  __device__ __forceinline__ Request() {}
+  __device__ __forceinline__ Request(const AttnArgs& a, int b) {
     const int s = sequence_of(a.c, a.seqs, b);
     n = a.n_new ? min(max(a.n_new[b], 0), a.N) : a.N;
     len = 0;
     if (s >= 0) len = min(max(a.c.lens[s], 0), a.c.width << a.c.log_page);
     else n = 0;
-    const long rows = static_cast<long>(n) * a.group;
-    items = a.c.heads * static_cast<int>((rows + ROWS_PER_ITEM - 1) / ROWS_PER_ITEM);
-    tiles = (len + n + UNIT - 1) / UNIT;
+    blocks = (n + a.nodes - 1) / a.nodes;
+    const bool paired = !a.mask && blocks > 1;
+    pairs = paired ? (blocks + 1) / 2 : blocks;
+    per = paired ? (2u * len + static_cast<u32>(blocks + 1) * a.nodes + 2 * (kUnit - 1)) / kUnit : static_cast<u32>(len + n + kUnit - 1) / kUnit;
   }
-  __device__ __forceinline__ long units() const { return static_cast<long>(items) * tiles; }
+  __device__ __forceinline__ u32 units(const AttnArgs& a) const { return static_cast<u32>(a.c.heads) * pairs * per; }
+  // Keys that a block's rows see at most.
+  __device__ __forceinline__ int keys(const AttnArgs& a, int block) const { return len + (a.mask ? n : min(n, (block + 1) * a.nodes)); }
+  __device__ __forceinline__ u32 block_units(const AttnArgs& a, int block) const { return static_cast<u32>(keys(a, block) + kUnit - 1) / kUnit; }
 };
-// Units in front of every request, in LDS: sh[b], b <= B.  All threads of a work-group of kThreads.
-template <typename D> __device__ __forceinline__ void deal_out(const AttnArgs& a, u32* sh) {
-  __shared__ u32 sums[kThreads / kWave];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  u32 front = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-    const int b = b0 + threadIdx.x;
-    const u32 v = b < a.B ? static_cast<u32>(D(a, b).units()) : 0;
-    u32 x = v;
+// Units before the one a place in the deal begins with, sums over a wave's lanes.
+__device__ __forceinline__ u32 wave_scan(u32 v) {
+  const int lane = threadIdx.x % kWave;
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const u32 y = __shfl_up(x, d);
-      if (lane >= d) x += y;
-    }
-    if (lane == kWave - 1) sums[wave] = x;
-    __syncthreads();
-    u32 total = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / kWave; ++w) {
-      if (w < wave) x += sums[w];
-      total += sums[w];
-    }
-    if (b < a.B) sh[b] = front + x - v;
-    front += total;
-    __syncthreads();
+  for (int d = 1; d < kWave; d <<= 1) {
+    const u32 y = __shfl_up(v, d);
+    if (lane >= d) v += y;
   }
-  if (threadIdx.x == 0) sh[a.B] = front;
-  __syncthreads();
+  return v;
 }
-// The request that unit u belongs to: the last b with sh[b] <= u (requests without units never are).
-__device__ __forceinline__ int request_of(const u32* sh, int B, u32 u) {
-  int lo = 0, hi = B - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (sh[mid] <= u) lo = mid;
-    else hi = mid - 1;
+// A place in the deal, kept by every wave for itself: 64 requests at a time, one per lane.
+struct Deal {
+  const AttnArgs& a;
+  Request mine;       // of request first + lane
+  int first;
+  u32 front, before;  // units in front of the 64, in front of the lane's request
+  u32 sum;            // of the 64
+  u32 total;
+  __device__ __forceinline__ void load(int b0, u32 units_in_front) {
+    first = b0;
+    front = units_in_front;
+    const int b = b0 + threadIdx.x % kWave;
+    mine = Request(a, min(b, a.B - 1));
+    const u32 units = b < a.B ? mine.units(a) : 0;
+    const u32 x = wave_scan(units);
+    before = front + x - units;
+    sum = __builtin_amdgcn_readlane(x, kWave - 1);
   }
-  return lo;
-}
+  __device__ __forceinline__ explicit Deal(const AttnArgs& args) : a(args) {
+    load(0, 0);
+    total = sum;
+    for (int b = kWave; b < a.B; b += kWave) {
+      const int b1 = b + threadIdx.x % kWave;
+      const u32 units = b1 < a.B ? Request(a, b1).units(a) : 0;
+      total += __builtin_amdgcn_readlane(wave_scan(units), kWave - 1);
+    }
+  }
+  // The block that unit u (not before an earlier call's) belongs to.
+  struct Place {
+    int b, head, block;
+    u32 begin, count;   // of the block in the deal; count = 0: idle
+    u32 offset;         // of u in the block; of idle ones: how many there are from u on
+    Request r;
+  };
+  __device__ __forceinline__ Place find(u32 u) {
+    while (u >= front + sum) load(first + kWave, front + sum);  // (u < total: there are more)
+    const unsigned long long at = __ballot(before <= u && first + static_cast<int>(threadIdx.x % kWave) < a.B);
+    // the last that begins at u or before; those without units that begin there too come before it or not at all
+    const int lane = 63 - __builtin_clzll(at);
+    Place p;
+    p.b = first + lane;
+    p.r.n = __builtin_amdgcn_readlane(mine.n, lane);
+    p.r.len = __builtin_amdgcn_readlane(mine.len, lane);
+    p.r.blocks = __builtin_amdgcn_readlane(mine.blocks, lane);
+    p.r.pairs = __builtin_amdgcn_readlane(mine.pairs, lane);
+    p.r.per = __builtin_amdgcn_readlane(mine.per, lane);
+    const u32 local = u - __builtin_amdgcn_readlane(before, lane);
+    const u32 item = local / p.r.per, in = local % p.r.per;
+    p.head = item / p.r.pairs;
+    p.block = item % p.r.pairs;
+    p.offset = in;
+    if (p.r.pairs == p.r.blocks) {  // (one block alone is no pair)
+      p.count = p.r.per;
+    } else {
+      const int late = p.r.blocks - 1 - p.block;
+      const u32 those = p.r.block_units(a, late);
+      if (in < those) {
+        p.block = late;
+        p.count = those;
+      } else {
+        p.offset = in - those;
+        p.count = late == p.block ? 0 : p.r.block_units(a, p.block);
+        if (p.offset >= p.count) {
+          p.count = 0;
+          p.offset = p.r.per - in;
+        }
+      }
+    }
+    p.begin = u - p.offset;
+    return p;
+  }
+};
 __device__ __forceinline__ u32 share_of(u32 total, u32 groups, u32 least) { return max((total + groups - 1) / groups, least); }
 
-// What a lane has of a tile, as it came from memory.
+// ---------------------------------------------------------------- tiles on their way through LDS
+// A tile of 32 keys in LDS: codes of the keys, codes of the values, then the scales of both.  Sixteen bytes go from memory to LDS per lane and
+// instruction, past the registers, to places that follow each other; which sixteen they are is chosen so that the reads below find
+// sixteen lanes' pieces on sixteen different groups of four banks.
 template <int D> struct Tile {
+  static constexpr int kCodes = 16 * D, kScales = D <= 128 ? 256 : 512;  // bytes
+  static constexpr int kBytes = 2 * kCodes + kScales;
+  static constexpr int kCodeLoads = kCodes / 1024, kScaleLoads = kScales / 256;
+  static constexpr int kLoads = 2 * kCodeLoads + kScaleLoads;
   static constexpr int S = D / 32, VW = D == 256 ? 16 : 8;
+  // Where sixteen bytes of the keys' codes stand: piece p (of D/32) of token t.
+  __device__ static __forceinline__ u32 key_slot(u32 t, u32 p) {
+    if (D == 64) return (t ^ (t >> 1 & 4)) * 2 + (p ^ (t >> 4 & 1));
+    if (D == 128) return t * 4 + (p ^ (t >> 3 & 3));
+    return t * 8 + (p ^ (t >> 2 & 6) ^ (t >> 1 & 1));
+  }
+  // And which piece of which token stands at `slot`: offset in the page's codes (from the tile's first token on).
+  __device__ static __forceinline__ u32 key_source(u32 slot) {
+    if (D == 64) {
+      const u32 row = slot >> 1, t = row ^ (row >> 1 & 4);
+      return t * 32 + ((slot & 1) ^ (t >> 4 & 1)) * 16;
+    }
+    if (D == 128) {
+      const u32 t = slot >> 2;
+      return t * 64 + ((slot & 3) ^ (t >> 3 & 3)) * 16;
+    }
+    const u32 t = slot >> 3;
+    return t * 128 + ((slot & 7) ^ (t >> 2 & 6) ^ (t >> 1 & 1)) * 16;
+  }
+  // The same for the values: half h of dword column c (its eight tokens) of octet o.
+  __device__ static __forceinline__ u32 value_slot(u32 o, u32 c, u32 h) {
+    if (D == 64) return (o * 8 + c) * 2 + h;
+    if (D == 128) return (o * 16 + c) * 2 + (h ^ (c >> 3));
+    return (o * 16 + (c >> 1)) * 4 + ((((c & 1) << 1) | h) ^ (c >> 3));
+  }
+  __device__ static __forceinline__ u32 value_source(u32 slot) {
+    if (D == 64) return slot * 16;
+    if (D == 128) return (slot ^ (slot >> 4 & 1)) * 16;
+    return (slot ^ (slot >> 4 & 3)) * 16;
+  }
+};
+__device__ __forceinline__ u32 lds_address(const void* p) {
+  return static_cast<u32>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p));
+}
+// To LDS from byte address `lds` on, lane after lane.  (Written by hand: behind the compiler's own form of these loads every read of
+// LDS waits for all that is in flight.  The wait states: a scalar operand can come from a vector instruction just before.)
+template <int BYTES> __device__ __forceinline__ void buffer_to_lds(__amdgpu_buffer_rsrc_t rows, u32 at, u32 base, u32 lds) {
+  if constexpr (BYTES == 16)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(at), "s"(rows), "s"(base) : "memory", "m0");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(at), "s"(rows), "s"(base) : "memory", "m0");
+}
+template <int BYTES> __device__ __forceinline__ void global_to_lds(const uint8_t* at, u32 lds) {
+  if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at) : "memory", "m0");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(at) : "memory", "m0");
+}
+template <int LEFT> __device__ __forceinline__ void arrived() {  // all loads of this wave but the last LEFT
+  static_assert(LEFT >= 0 && LEFT < 64, "the counter's range");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
+}
+constexpr int kBufferFlags = 0x00020000;  // untyped buffer, 32-bit data format
+
+// Fetches a wave's tiles of one piece of work, unit after unit.  UNIFORM: pages of 32 tokens and more, so that a tile lies in one page (a
+// buffer, which the loads cannot leave).  Otherwise an octet does.  The page numbers of the next units lie in one register, a lane each: a load of the
+// compiler's own in every unit would be waited for together with all that is in flight.
+template <int D, bool UNIFORM> struct Fetch {
+  using X = Tile<D>;
+  static constexpr int kSpan = UNIFORM ? kWave : kWave / 4;  // units whose pages are known at a time
+  const AttnArgs& a;
+  const int32_t* row;  // of the page table
+  int head, end, t0;   // keys there are; the next tile's first
+  int ids, at;         // pages, which of them is next
+  __device__ __forceinline__ Fetch(const AttnArgs& a_, int s, int head_, int end_, int from)
+      : a(a_), row(a_.c.page_table + static_cast<size_t>(s) * a_.c.width), head(head_), end(end_), t0(from) {
+    look_up();
+  }
+  // (past the end: the last position's page; -1 past the table)
+  __device__ __forceinline__ void look_up() {
+    const int lane = threadIdx.x % kWave, t = UNIFORM ? t0 + lane * kUnit : t0 + lane / 4 * kUnit + lane % 4 * 8;
+    const int i = min(t, end - 1) >> a.c.log_page;
+    ids = i < a.c.width ? row[i] : -1;
+    asm volatile("" : "+v"(ids));  // waited for here, and not wherever it is next read
+    at = 0;
+  }
+  // Octet (of the tile's four) that a lane's share of load i of the codes, or of the scales, belongs to.
+  __device__ static __forceinline__ int code_octet(int i) { return (i * kWave + static_cast<int>(threadIdx.x % kWave)) / (D / 4); }
+  __device__ static __forceinline__ int scale_octet() {
+    const int lane = threadIdx.x % kWave;
+    return D == 256 ? lane / 16 : D == 128 ? lane % 32 / 8 : lane % 16 / 4;
+  }
+  // The next tile to LDS.  Returns which of its octets have no page (bit by bit).
+  __device__ __forceinline__ u32 next(u32 lds) {
+    if (at == kSpan) look_up();
+    const u32 lane = threadIdx.x % kWave, lp = a.c.log_page, in_page = (1u << lp) - 1;
+    u32 bad;
+    if constexpr (UNIFORM) {
+      const u32 id = __builtin_amdgcn_readlane(ids, at);
+      bad = id >= static_cast<u32>(a.c.pages) ? 0xF : 0;
+      const auto rows = __builtin_amdgcn_make_buffer_rsrc(head_of(a.c, a.layer_offset, bad ? 0 : id, head), 0, static_cast<int>(a.c.blk), kBufferFlags);
+      const u32 t = static_cast<u32>(t0) & in_page, k0 = t * (D / 2), v0 = ((D / 2) << lp) + k0;
+#pragma unroll
+      for (int i = 0; i < X::kCodeLoads; ++i) buffer_to_lds<16>(rows, X::key_source(i * kWave + lane), k0, lds + i * 1024);
+#pragma unroll
+      for (int i = 0; i < X::kCodeLoads; ++i) buffer_to_lds<16>(rows, X::value_source(i * kWave + lane), v0, lds + X::kCodes + i * 1024);
+      const u32 s0 = (D << lp) + t * (D / 32), of_values = (D / 32) << lp;
+      if constexpr (D == 256) {
+        buffer_to_lds<4>(rows, lane * 4, s0, lds + 2 * X::kCodes);
+        buffer_to_lds<4>(rows, lane * 4, s0 + of_values, lds + 2 * X::kCodes + 256);
+      } else {  // the keys' scales in lanes 0 .. 31 (D = 64: twice), the values' in the others
+        buffer_to_lds<4>(rows, lane % (D / 4) * 4 + lane / 32 * of_values, s0, lds + 2 * X::kCodes);
+      }
+    } else {
+      bad = __ballot(static_cast<u32>(ids) >= static_cast<u32>(a.c.pages)) >> (at * 4) & 0xF;
+      const u32 last = static_cast<u32>(end - 1) & ~7u;  // (octets past the end: the last one's place)
+      auto head_at = [&](int octet) {
+        const int p = __shfl(ids, at * 4 + octet);
+        return head_of(a.c, a.layer_offset, static_cast<u32>(p) < static_cast<u32>(a.c.pages) ? p : 0, head);
+      };
+#pragma unroll
+      for (int i = 0; i < X::kCodeLoads; ++i) {
+        const u32 o = code_octet(i), t = min(static_cast<u32>(t0) + 8 * o, last) & in_page;
+        const uint8_t* at = head_at(o) + t * (D / 2) - o * (4 * D);
+        global_to_lds<16>(at + X::key_source(i * kWave + lane), lds + i * 1024);
+        global_to_lds<16>(at + ((D / 2) << lp) + X::value_source(i * kWave + lane), lds + X::kCodes + i * 1024);
+      }
+      const u32 o = scale_octet(), t = min(static_cast<u32>(t0) + 8 * o, last) & in_page;
+      const uint8_t* scales = head_at(o) + (D << lp) + t * (D / 32) + lane % (D / 16) * 4;
+      if constexpr (D == 256) {
+        global_to_lds<4>(scales, lds + 2 * X::kCodes);
+        global_to_lds<4>(scales + ((D / 32) << lp), lds + 2 * X::kCodes + 256);
+      } else {
+        global_to_lds<4>(scales + (lane >= 32 ? (D / 32) << lp : 0), lds + 2 * X::kCodes);
+      }
+    }
+    t0 += kUnit;
+    ++at;
+    return bad;
+  }
+};
+// What a lane has of a tile, in registers.
+template <int D> struct Share {
+  static constexpr int S = D / 32, VW = Tile<D>::VW;
   u32 k[2][S], ks[2], v[VW];
   u32x2 vs;
+  __device__ __forceinline__ explicit Share(const uint8_t* tile) {
+    using X = Tile<D>;
+    const u32 lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
+    const uint8_t* scales = tile + 2 * X::kCodes;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const u32 t = (r >> 2) * 8 + 4 * b + (r & 3);
+      if constexpr (D == 64) {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(tile + X::key_slot(t, g >> 1) * 16 + (g & 1) * 8);
+        k[b][0] = w[0]; k[b][1] = w[1];
+        ks[b] = scales[t * 2 + (g >> 1)];
+      } else {
+#pragma unroll
+        for (int h = 0; h < D / 128; ++h) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(tile + X::key_slot(t, 4 * h + g) * 16);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) k[b][4 * h + j] = w[j];
+        }
+        if constexpr (D == 128) ks[b] = scales[t * 4 + g];
+        else ks[b] = scales[t * 8 + g] | static_cast<u32>(scales[t * 8 + 4 + g]) << 8;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VW / 4; ++i) {
+      const u32 c = D == 64 ? r >> 1 : D == 128 ? r : 2 * r + (i >> 1);
+      const u32x4 w = *reinterpret_cast<const u32x4*>(tile + X::kCodes + X::value_slot(g, c, i & 1) * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[4 * i + j] = w[j];
+    }
+    vs = *reinterpret_cast<const u32x2*>(scales + (D <= 128 ? 128 : 256) + g * (D / 4) + (r * (D / 16)) / 32 * 8);
+  }
 };
 
-// A wave's rows, their queries and what it has gathered for them.
+// ---------------------------------------------------------------- a wave's rows
+// Channels of the queries (and keys) that lane group g takes in step s: eight from here on.
+template <int D> __device__ __forceinline__ int channel(int g, int s) { return D == 64 ? g * 16 + s * 8 : s / 4 * 128 + g * 32 + s % 4 * 8; }
+
 template <int D, int RB, typename T> struct Wave {
   static constexpr int S = D / 32;              // steps of 32 channels
   static constexpr int NF = D / 16;             // blocks of 16 channels of the result
@@ -152,19 +381,20 @@ template <int D, int RB, typename T> struct Wave {
   float m[RB], l[RB];
   int node[RB];                                 // of this lane's rows; < 0: no row
 
-  __device__ __forceinline__ void start(const AttnArgs& a, int b, int head, int row0, int rows) {
+  // Rows row0 .. of the block of nodes from node0 on, which has `rows`.
+  __device__ __forceinline__ void start(const AttnArgs& a, int b, int head, int node0, int row0, int rows) {
     const int lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const int row = row0 + rb * 16 + r;
       const bool live = row < rows;
-      node[rb] = live ? row / a.group : -1;
-      const T* at = static_cast<const T*>(a.q) + b * a.q_request + static_cast<long>(live ? node[rb] : 0) * a.q_node +
-                    static_cast<long>(head * a.group + (live ? row - node[rb] * a.group : 0)) * a.q_head + g * (D / 4);
+      const int in = live ? row / a.group : 0, h = live ? row - in * a.group : 0;
+      node[rb] = live ? node0 + in : -1;
+      const T* at = static_cast<const T*>(a.q) + b * a.q_request + static_cast<long>(node0 + in) * a.q_node + static_cast<long>(head * a.group + h) * a.q_head;
 #pragma unroll
       for (int s = 0; s < S; ++s) {
         u32 t[4][TERMS];
-        const Eight e = load_eight(at + s * 8);
+        const Eight e = load_eight(at + channel<D>(g, s));
 #pragma unroll
         for (int p = 0; p < 4; ++p) split_pair<TERMS>(live ? e.x[2 * p] : 0.0f, live ? e.x[2 * p + 1] : 0.0f, t[p]);
 #pragma unroll
@@ -178,64 +408,32 @@ template <int D, int RB, typename T> struct Wave {
   }
 };
 
-// Where the lane finds its keys and values: requests' pages, one tile after the other.
-template <int D> struct Reader {
-  const AttnArgs& a;
-  const int32_t* row;       // of the page table
-  int head, end;            // keys there are
-  __device__ __forceinline__ Reader(const AttnArgs& a_, int s, int head_, int end_)
-      : a(a_), row(a_.c.page_table + static_cast<size_t>(s) * a_.c.width), head(head_), end(end_) {}
-  // The page that holds position t (past the end: the last position); -1 past the table.
-  __device__ __forceinline__ int page(int t) const {
-    const int i = min(t, end - 1) >> a.c.log_page;
-    return i < a.c.width ? row[i] : -1;
-  }
-  __device__ __forceinline__ void load(int t0, int kpage, int vpage, Tile<D>& x) const {
-    const int lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
-    const u32 in_page = (1u << a.c.log_page) - 1, last = static_cast<u32>(end - 1) & ~7u;
-    const u32 kp = static_cast<u32>(kpage) < static_cast<u32>(a.c.pages) ? kpage : 0, vp = static_cast<u32>(vpage) < static_cast<u32>(a.c.pages) ? vpage : 0;
-    const uint8_t* kb = head_of(a.c, a.layer_offset, kp, head);
-    const u32 kt = (min(static_cast<u32>(t0) + (r >> 2) * 8, last) & in_page) + (r & 3);
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const uint8_t* at = kb + Place<D>::key(kt + 4 * b) + g * (D / 8);
-      if constexpr (D == 64) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(at);
-        x.k[b][0] = w[0]; x.k[b][1] = w[1];
-      } else {
-#pragma unroll
-        for (int i = 0; i < D / 128; ++i) {
-          const u32x4 w = reinterpret_cast<const u32x4*>(at)[i];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x.k[b][4 * i + j] = w[j];
-        }
-      }
-      const uint8_t* st = kb + Place<D>::key_scale(a.c.log_page, kt + 4 * b);
-      if constexpr (D == 256) x.ks[b] = *reinterpret_cast<const uint16_t*>(st + 2 * g);
-      else x.ks[b] = st[D == 64 ? g >> 1 : g];
-    }
-    const uint8_t* vb = head_of(a.c, a.layer_offset, vp, head);
-    const u32 vt = min(static_cast<u32>(t0) + g * 8, last) & in_page;
-    const u32 column = D == 64 ? r >> 1 : D == 128 ? r : 2 * r;
-    const u32x4* at = reinterpret_cast<const u32x4*>(vb + Place<D>::value(a.c.log_page, vt) + column * 32);
-#pragma unroll
-    for (int i = 0; i < Tile<D>::VW / 4; ++i) {
-      const u32x4 w = at[i];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x.v[4 * i + j] = w[j];
-    }
-    x.vs = *reinterpret_cast<const u32x2*>(vb + Place<D>::value_scale(a.c.log_page, vt) + (r * (D / 16)) / 32 * 8);
-  }
-};
-
 // Two keys' values of the same channel beside each other: the low halves of two conversions, or the high ones.
 __device__ __forceinline__ u32 low_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// `sees[rb]`: of keys 8g .. 8g + 7 of the tile, which the lane's row sees (bit by bit); only looked at where MASKED.
-// `poison`: the lane's octet has no page.
-template <int D, int RB, typename T, bool MASKED>
-__device__ __forceinline__ void attend(Wave<D, RB, T>& w, const Tile<D>& x, float c, const u32 (&sees)[RB], int there, bool poison) {
+// Which of the keys first .. first + 7 (numbered from the first node on; committed ones are < 0) row `node` of n nodes sees.
+__device__ __forceinline__ u32 seen(const AttnArgs& a, int b, int node, int n, int first) {
+  u32 bits;
+  if (a.mask) {
+    const unsigned long long* row = a.mask + (static_cast<size_t>(b) * a.N + node) * a.words;
+    auto word = [&](int w) { return w < 0 ? ~0ull : w < a.words ? row[w] : 0ull; };
+    const int w = first >> 6, shift = first & 63;
+    bits = static_cast<u32>(word(w) >> shift);
+    if (shift > 56) bits |= static_cast<u32>(word(w + 1) << (64 - shift));
+  } else {
+    const int k = node + 1 - first;
+    bits = k >= 8 ? 0xFFu : k <= 0 ? 0u : (1u << k) - 1;
+  }
+  const int k = n - first;
+  return bits & (k >= 8 ? 0xFFu : k <= 0 ? 0u : (1u << k) - 1);
+}
+
+// One tile.  `plain` (the same for the wave): every row sees all of it, and all of it is there.  Otherwise: request b has n nodes behind
+// `len` tokens, the tile begins at t0; `poison`: the lane's octet has no page.
+template <int D, int RB, typename T>
+__device__ __forceinline__ void attend(const AttnArgs& a, Wave<D, RB, T>& w, const Share<D>& x, bool plain, int b, int len, int n, int t0, bool poison) {
+  const float c = a.scale_log2;
   constexpr int S = D / 32, NF = D / 16, TERMS = Wave<D, RB, T>::TERMS;
   const int lane = threadIdx.x % kWave, r = lane % 16;
   f32x4 sc[2][RB];
@@ -243,7 +441,7 @@ __device__ __forceinline__ void attend(Wave<D, RB, T>& w, const Tile<D>& x, floa
   for (int b = 0; b < 2; ++b) {
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) sc[b][rb] = f32x4{0, 0, 0, 0};
-    const u32 s0 = x.ks[b] << 23, s1 = D == 256 ? x.ks[b] << 15 : s0;
+    const u32 s0 = scale_at<0>(x.ks[b]), s1 = D == 256 ? scale_at<1>(x.ks[b]) : s0;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const u32 scale = s < 4 ? s0 : s1;
@@ -254,16 +452,25 @@ __device__ __forceinline__ void attend(Wave<D, RB, T>& w, const Tile<D>& x, floa
         for (int t = TERMS - 1; t >= 0; --t) sc[b][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, w.q[t][rb][s], sc[b][rb], 0, 0, 0);
     }
   }
-  if (MASKED) {
+  __builtin_amdgcn_sched_barrier(0);  // (the values' conversions would be brought up to here, and their results kept)
+  u32 vs0 = x.vs[0], vs1 = x.vs[1];  // scales of the eight keys
+  if (!plain) {
+    const int first = t0 + lane / 16 * 8 - len;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
+    for (int rb = 0; rb < RB; ++rb) {
+      const u32 sees = w.node[rb] < 0 ? 0u : seen(a, b, w.node[rb], n, first);
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float s = poison ? __builtin_nanf("") : sc[b][rb][i];
-          sc[b][rb][i] = sees[rb] >> (4 * b + i) & 1 ? s : -__builtin_inff();
+          const float s = poison ? __builtin_nanf("") : sc[k][rb][i];
+          sc[k][rb][i] = sees >> (4 * k + i) & 1 ? s : -__builtin_inff();
         }
+    }
+    // past the end of the sequence memory holds anything, and 0 times that has to be 0
+    const int there = n - first;  // of the lane's eight keys
+    vs0 = there >= 4 ? vs0 : there <= 0 ? 0 : vs0 & ((1u << (8 * there)) - 1);
+    vs1 = there >= 8 ? vs1 : there <= 4 ? 0 : vs1 & ((1u << (8 * (there - 4))) - 1);
   }
   float top[RB];
   bool up = false;
@@ -301,16 +508,10 @@ __device__ __forceinline__ void attend(Wave<D, RB, T>& w, const Tile<D>& x, floa
       for (int k = 0; k < TERMS; ++k) p[k][rb][h] = t[k];
     }
   }
-  // scales of the eight keys; past the end of the sequence memory holds anything, and 0 times that has to be 0
+  __builtin_amdgcn_sched_barrier(0);
   u32 vs[8];
-  u32 s0 = x.vs[0], s1 = x.vs[1];
-  if (MASKED) {
-    const int n = there;  // of the lane's eight keys
-    s0 = n >= 4 ? s0 : n <= 0 ? 0 : s0 & ((1u << (8 * n)) - 1);
-    s1 = n >= 8 ? s1 : n <= 4 ? 0 : s1 & ((1u << (8 * (n - 4))) - 1);
-  }
-  vs[0] = scale_at<0>(s0); vs[1] = scale_at<1>(s0); vs[2] = scale_at<2>(s0); vs[3] = scale_at<3>(s0);
-  vs[4] = scale_at<0>(s1); vs[5] = scale_at<1>(s1); vs[6] = scale_at<2>(s1); vs[7] = scale_at<3>(s1);
+  vs[0] = scale_at<0>(vs0); vs[1] = scale_at<1>(vs0); vs[2] = scale_at<2>(vs0); vs[3] = scale_at<3>(vs0);
+  vs[4] = scale_at<0>(vs1); vs[5] = scale_at<1>(vs1); vs[6] = scale_at<2>(vs1); vs[7] = scale_at<3>(vs1);
   auto product = [&](int f, u32 v0, u32 v1, u32 v2, u32 v3) {
     const bf16x8 v = as_bf16x8(v0, v1, v2, v3);
 #pragma unroll
@@ -342,31 +543,14 @@ __device__ __forceinline__ void attend(Wave<D, RB, T>& w, const Tile<D>& x, floa
   }
 }
 
-// Which of the keys first .. first + 7 (numbered from the first node on; committed ones are < 0) row `node` of n nodes sees.
-__device__ __forceinline__ u32 seen(const AttnArgs& a, int b, int node, int n, int first) {
-  u32 bits;
-  if (a.mask) {
-    const unsigned long long* row = a.mask + (static_cast<size_t>(b) * a.N + node) * a.words;
-    auto word = [&](int w) { return w < 0 ? ~0ull : w < a.words ? row[w] : 0ull; };
-    const int w = first >> 6, shift = first & 63;
-    bits = static_cast<u32>(word(w) >> shift);
-    if (shift > 56) bits |= static_cast<u32>(word(w + 1) << (64 - shift));
-  } else {
-    const int k = node + 1 - first;
-    bits = k >= 8 ? 0xFFu : k <= 0 ? 0u : (1u << k) - 1;
-  }
-  const int k = n - first;
-  return bits & (k >= 8 ? 0xFFu : k <= 0 ? 0u : (1u << k) - 1);
-}
-
 // Where the results of a lane go: element [f][i] of row rb is channel (4g + i) * D/16 + f.
 template <int D, int RB, typename T>
-__device__ __forceinline__ void write_rows(const AttnArgs& a, int b, int head, int row0, int rb, int rows, const f32x4 (&o)[D / 16], float m, float l) {
+__device__ __forceinline__ void write_rows(const AttnArgs& a, int b, int head, int node0, int row0, int rb, int rows, const f32x4 (&o)[D / 16], float m, float l) {
   constexpr int C = D / 16;
   const int lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
   const int row = row0 + rb * 16 + r;
   if (row >= rows) return;
-  const int node = row / a.group, h = head * a.group + row - node * a.group;
+  const int in = row / a.group, node = node0 + in, h = head * a.group + row - in * a.group;
   const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
   T* at = static_cast<T*>(a.out) + b * a.out_request + node * a.out_node + h * a.out_head + g * (4 * C);
 #pragma unroll
@@ -415,103 +599,89 @@ template <typename T, int D> __device__ __forceinline__ void clear_rows(const At
 }
 
 enum { KEYS = 0, ROWS = 1 };  // what the waves of a work-group divide between them
-template <int MODE, int RB> constexpr int rows_per_item = MODE == KEYS ? 16 * RB : 64 * RB;
-template <int MODE> constexpr int unit_keys = MODE == KEYS ? 4 * kTile : kTile;
-
-// One wave over keys [from, to) of an item; every `step`-th tile of 32 from `from` on.
-template <int D, int RB, typename T>
-__device__ __forceinline__ void run_keys(const AttnArgs& a, Wave<D, RB, T>& w, int b, int s, int head, int len, int n, int from, int to, int step) {
-  const int lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
-  const int end = len + n;
-  // rows of a wave without a mask see nothing past their last node
-  int last = end;
-  if (!a.mask) {
-    int node = -1;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) node = max(node, w.node[rb]);
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) node = max(node, __shfl_xor(node, d));
-    last = min(end, len + 1 + __builtin_amdgcn_readfirstlane(node));
-  }
-  to = min(to, last);
-  if (from >= to) return;
-  const Reader<D> reader(a, s, head, end);
-  Tile<D> x, next;
-  int kpage = reader.page(from + (r >> 2) * 8), vpage = reader.page(from + g * 8);
-  reader.load(from, kpage, vpage, next);
-  int next_vpage = vpage;
-  if (from + step < to) {
-    kpage = reader.page(from + step + (r >> 2) * 8);
-    vpage = reader.page(from + step + g * 8);
-  }
-  for (int t0 = from; t0 < to; t0 += step) {
-    x = next;
-    const bool poison = static_cast<u32>(next_vpage) >= static_cast<u32>(a.c.pages);
-    if (t0 + step < to) {
-      reader.load(t0 + step, kpage, vpage, next);
-      next_vpage = vpage;
-      if (t0 + 2 * step < to) {
-        kpage = reader.page(t0 + 2 * step + (r >> 2) * 8);
-        vpage = reader.page(t0 + 2 * step + g * 8);
-      }
-    }
-    u32 sees[RB];
-    if (t0 + kTile <= len && !__any(poison)) {
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) sees[rb] = 0xFF;
-      attend<D, RB, T, false>(w, x, a.scale_log2, sees, 8, false);
-    } else {
-      const int first = t0 + 8 * g;
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) sees[rb] = w.node[rb] < 0 ? 0u : seen(a, b, w.node[rb], n, first - len);
-      attend<D, RB, T, true>(w, x, a.scale_log2, sees, end - first, poison);
-    }
-  }
+template <int MODE, int RB> constexpr int rows_per_block = MODE == KEYS ? 16 * RB : 64 * RB;
+// Work-groups that have to fit a compute unit beside each other: what the compiler may give a wave of registers, and the ring of LDS.
+template <int D, int RB, typename T> constexpr int per_unit = D == 256 ? (RB == 1 && !std::is_same<T, float>::value ? 2 : 1) : std::is_same<T, float>::value ? 2 : RB == 1 ? 3 : 2;
+constexpr int stages_of(int D, int groups) {  // units in the ring, the one that is worked on among them
+  const int n = (160 * 1024 / groups - 1024) / (kWaves * (32 * D + (D <= 128 ? 256 : 512)));
+  return n > 4 ? 4 : n;
 }
 
-template <int D, int RB, typename T, int MODE>
-__global__ void __launch_bounds__(kThreads) attention_kernel(AttnArgs a, u32 least) {
-  constexpr int NF = D / 16, ROWS_ITEM = rows_per_item<MODE, RB>, UNIT = unit_keys<MODE>;
-  using Dealt = Deal<ROWS_ITEM, UNIT>;
-  __shared__ u32 sh_begin[MARS_KV_MAX_REQUESTS + 1];
+template <int D, int RB, typename T, int MODE, bool UNIFORM>
+__global__ void __launch_bounds__(kThreads, (per_unit<D, RB, T>)) attention_kernel(AttnArgs a) {
+  using X = Tile<D>;
+  constexpr int NF = D / 16, STAGES = stages_of(D, per_unit<D, RB, T>);
+  static_assert(STAGES >= 2, "a unit in flight while another is worked on");
+  constexpr int kJoin = MODE == KEYS ? 2 * RB * NF * 1024 : 0;  // bytes for two waves' results
+  constexpr int kRing = STAGES * kWaves * X::kBytes;
+  __shared__ __attribute__((aligned(1024))) uint8_t sh_ring[kRing > kJoin ? kRing : kJoin];
+  __shared__ u32 sh_bad[STAGES][kWaves];
   __shared__ float sh_m[MODE == KEYS ? 4 : 1][16 * RB], sh_l[MODE == KEYS ? 4 : 1][16 * RB];
-  __shared__ __attribute__((aligned(16))) float sh_o[MODE == KEYS ? 2 : 1][MODE == KEYS ? RB * NF * 256 : 4];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
 
   if (a.n_new || a.seqs)  // (otherwise every request has N nodes)
     for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-      const Dealt d(a, b);
-      if (d.n < a.N) clear_rows<T, D>(a, b, d.n);
+      const int n = Request(a, b).n;
+      if (n < a.N) clear_rows<T, D>(a, b, n);
     }
-  deal_out<Dealt>(a, sh_begin);
-  const u32 total = sh_begin[a.B], share = share_of(total, gridDim.x, least);
+  Deal deal(a);
+  const u32 share = share_of(deal.total, gridDim.x, a.least);
   // neighbours in the deal on the same die (block index mod 8)
   const u32 per_die = gridDim.x >> 3;
   const u32 group = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3);
   const unsigned long long my_begin = static_cast<unsigned long long>(group) * share;
-  if (my_begin >= total) return;
-  const u32 unit0 = static_cast<u32>(my_begin), unit1 = static_cast<u32>(min(my_begin + share, static_cast<unsigned long long>(total)));
+  if (my_begin >= deal.total) return;
+  const u32 unit0 = static_cast<u32>(my_begin), unit1 = static_cast<u32>(min(my_begin + share, static_cast<unsigned long long>(deal.total)));
+  const u32 ring = lds_address(sh_ring);
 
   Wave<D, RB, T> w;
   for (u32 u = unit0; u < unit1;) {
-    const int b = request_of(sh_begin, a.B, u);
-    const Dealt d(a, b);
-    const u32 local = u - sh_begin[b];
-    const int item = static_cast<int>(local / d.tiles), tile = static_cast<int>(local % d.tiles);
-    const int tiles = static_cast<int>(min(static_cast<u32>(d.tiles - tile), unit1 - u));
-    const bool whole = tile == 0 && tiles == d.tiles;
-    const int blocks = d.items / a.c.heads;
-    const int head = item / blocks, block = item % blocks, rows = d.n * a.group;
-    const int row0 = block * ROWS_ITEM + (MODE == ROWS ? wave * 16 * RB : 0);
-    const int s = sequence_of(a.c, a.seqs, b);
-    w.start(a, b, head, row0, rows);
-    const int from = tile * UNIT + (MODE == KEYS ? wave * kTile : 0), to = (tile + tiles) * UNIT;
-    if (MODE == KEYS || row0 < rows) run_keys<D, RB, T>(a, w, b, s, head, d.len, d.n, from, to, UNIT);
+    const auto p = deal.find(u);
+    if (p.count == 0) {
+      u += p.offset;
+      continue;
+    }
+    const int units = static_cast<int>(min(p.count - p.offset, unit1 - u));
+    const bool whole = static_cast<u32>(units) == p.count;
+    const int node0 = p.block * a.nodes, rows = min(a.nodes, p.r.n - node0) * a.group, row0 = MODE == ROWS ? wave * 16 * RB : 0;
+    const int len = p.r.len, n = p.r.n, end = len + n;
+    // no row of this wave sees keys from here on (-1: it has no rows)
+    const int limit = row0 >= rows ? 0 : a.mask ? end : len + 1 + node0 + (min(rows, row0 + 16 * RB) - 1) / a.group;
+    const int from = static_cast<int>(p.offset) * kUnit;
+    // (in front of the queries' loads; LDS is free: the piece before ended with a barrier)
+    Fetch<D, UNIFORM> fetch(a, sequence_of(a.c, a.seqs, p.b), p.head, end, from + wave * kTile);
+    u32 stage = 0;
+    auto issue = [&](u32 to) {
+      const u32 bad = fetch.next(ring + (to * kWaves + wave) * X::kBytes);
+      if (lane == 0) sh_bad[to][wave] = bad;
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+      if (i < units) issue(i);
+    w.start(a, p.b, p.head, node0, row0, rows);
+
+    for (int unit = 0; unit < units; ++unit) {
+      // this wave's tile of the unit is there; with a barrier, all are, and nobody reads the unit before any more
+      if (unit + STAGES - 1 <= units) arrived<(STAGES - 2) * X::kLoads>();
+      else arrived<0>();
+      if (MODE == ROWS) __builtin_amdgcn_s_barrier();
+      if (unit + STAGES - 1 < units) issue(stage == 0 ? STAGES - 1 : stage - 1);
+      const int t_unit = from + unit * kUnit;
+#pragma unroll 1
+      for (int i = MODE == KEYS ? wave : 0; i < (MODE == KEYS ? wave + 1 : kWaves); ++i) {
+        const int t0 = t_unit + i * kTile;
+        if (t0 >= limit) break;
+        const u32 bad = __builtin_amdgcn_readfirstlane(sh_bad[stage][i]);
+        const Share<D> x(sh_ring + (stage * kWaves + i) * X::kBytes);
+        attend<D, RB, T>(a, w, x, t0 + kTile <= len && bad == 0, p.b, len, n, t0, bad >> g & 1);
+      }
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) w.l[rb] = over_groups_sum(w.l[rb]);
+    __syncthreads();  // the ring is free
 
     if (MODE == KEYS) {
-      __syncthreads();  // (the piece before)
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb)
         if (lane < 16) {
@@ -535,7 +705,7 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(AttnArgs a, u32 lea
       // waves 2 and 3 to 0 and 1, then 1 to 0
 #pragma unroll
       for (int half = 2; half >= 1; half >>= 1) {
-        f32x4* const sh = reinterpret_cast<f32x4*>(sh_o[wave & (half - 1)]) + lane;
+        f32x4* const sh = reinterpret_cast<f32x4*>(sh_ring) + (wave & (half - 1)) * (RB * NF * kWave) + lane;
         if (wave >= half && wave < 2 * half) {
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb)
@@ -559,7 +729,7 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(AttnArgs a, u32 lea
           f32x4 o[NF];
 #pragma unroll
           for (int f = 0; f < NF; ++f) o[f] = w.o[f][rb];
-          write_rows<D, RB, T>(a, b, head, row0, rb, rows, o, w.m[rb], w.l[rb]);
+          write_rows<D, RB, T>(a, p.b, p.head, node0, row0, rb, rows, o, w.m[rb], w.l[rb]);
         }
       } else {
         // the first piece of the group's run, or its last one
@@ -576,54 +746,47 @@ __global__ void __launch_bounds__(kThreads) attention_kernel(AttnArgs a, u32 lea
         }
       }
     }
-    u += tiles;
+    u += units;
   }
 }
 
-// Joins the pieces of items that were dealt to several work-groups: one work-group for every place where the deal cuts one, of which the
-// first of an item takes it; a wave per 16 rows.
+// Joins the pieces of blocks that were dealt to several work-groups: one work-group for every place where the deal cuts one, of which the
+// first of a block takes it; a wave per 16 rows and quarter of the channels.
 template <int D, int RB, typename T, int MODE>
-__global__ void __launch_bounds__(kThreads) merge_kernel(AttnArgs a, u32 groups, u32 least) {
-  constexpr int NF = D / 16, ROWS_ITEM = rows_per_item<MODE, RB>, UNIT = unit_keys<MODE>;
-  using Dealt = Deal<ROWS_ITEM, UNIT>;
-  __shared__ u32 sh_begin[MARS_KV_MAX_REQUESTS + 1];
-  deal_out<Dealt>(a, sh_begin);
-  const u32 total = sh_begin[a.B], share = share_of(total, groups, least);
+__global__ void __launch_bounds__(kThreads) merge_kernel(AttnArgs a, u32 groups) {
+  constexpr int NF = D / 16;
+  Deal deal(a);
+  const u32 share = share_of(deal.total, groups, a.least);
   const u32 cut = blockIdx.x + 1;
   const unsigned long long at = static_cast<unsigned long long>(cut) * share;
-  if (at >= total) return;
-  const int b = request_of(sh_begin, a.B, static_cast<u32>(at));
-  const Dealt d(a, b);
-  const u32 local = static_cast<u32>(at) - sh_begin[b];
-  const int item = static_cast<int>(local / d.tiles);
-  const u32 item0 = sh_begin[b] + static_cast<u32>(item) * d.tiles, item1 = item0 + d.tiles;
-  if (item0 == at) return;                            // cut between two items
-  const u32 first = item0 / share, last = (item1 - 1) / share;
+  if (at >= deal.total) return;
+  const auto p = deal.find(static_cast<u32>(at));
+  if (p.count == 0 || p.begin == at) return;          // cut between two blocks
+  const u32 first = p.begin / share, last = (p.begin + p.count - 1) / share;
   if (cut != first + 1) return;                       // an earlier cut's
-  const int blocks = d.items / a.c.heads;
-  const int head = item / blocks, block = item % blocks, rows = d.n * a.group;
+  const int node0 = p.block * a.nodes, rows = min(a.nodes, p.r.n - node0) * a.group;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 16;
   constexpr int STRIPS = MODE == ROWS ? 4 * RB : RB;   // of 16 rows
   for (int strip = blockIdx.y * 4 + wave; strip < STRIPS; strip += gridDim.y * 4) {
     const int part = MODE == ROWS ? strip / RB : 0, rb = MODE == ROWS ? strip % RB : strip;
     auto slot = [&](u32 group) {
-      const u32 second = static_cast<unsigned long long>(group) * share >= item0 ? 0 : 1;
+      const u32 second = static_cast<unsigned long long>(group) * share >= p.begin ? 0 : 1;
       return (static_cast<long>(group) * 2 + second) * (MODE == ROWS ? 4 : 1) + part;
     };
     float m = kFloor;
-    for (u32 p = first; p <= last; ++p) m = fmaxf(m, Piece<D, RB>(a.partial, slot(p)).reference(rb * 16 + r));
+    for (u32 x = first; x <= last; ++x) m = fmaxf(m, Piece<D, RB>(a.partial, slot(x)).reference(rb * 16 + r));
     float l = 0.0f;
     f32x4 o[NF];
 #pragma unroll
     for (int f = 0; f < NF; ++f) o[f] = f32x4{0, 0, 0, 0};
-    for (u32 p = first; p <= last; ++p) {
-      const Piece<D, RB> piece(a.partial, slot(p));
+    for (u32 x = first; x <= last; ++x) {
+      const Piece<D, RB> piece(a.partial, slot(x));
       const float weight = __builtin_amdgcn_exp2f(piece.reference(rb * 16 + r) - m);
       l += piece.sum(rb * 16 + r) * weight;
 #pragma unroll
       for (int f = 0; f < NF; ++f) o[f] += piece.part(rb, f, lane) * weight;
     }
-    write_rows<D, RB, T>(a, b, head, block * ROWS_ITEM + part * 16 * RB, rb, rows, o, m, l);
+    write_rows<D, RB, T>(a, p.b, p.head, node0, part * 16 * RB, rb, rows, o, m, l);
   }
 }
 
