@@ -62,13 +62,12 @@ static int row_octets(int N) { return (N + 6) / 8 + 1; }  // octets that N posit
 struct AttnPlan {
   int mode, blocks_rb;  // waves divide keys or rows; blocks of 16 rows per wave
   int nodes;            // of a block of rows
-  u32 groups, least;    // work-groups; least units each takes
+  u32 groups;           // work-groups beside each other on the chip
   size_t bytes;         // of pieces
 };
 static size_t piece_bytes(int dim, int rb) { return sizeof(float) * (32 * rb + static_cast<size_t>(rb) * (dim / 16) * 256); }
 
-static AttnPlan attn_plan(int B, int N, int group, int dim, int dtype) {
-  (void)B;
+static AttnPlan attn_plan(int N, int group, int dim, int dtype) {
   const long rows = static_cast<long>(N) * group;
   AttnPlan p;
   p.mode = KEYS;
@@ -83,18 +82,20 @@ static AttnPlan attn_plan(int B, int N, int group, int dim, int dtype) {
     p.blocks_rb = 2;
     p.mode = ROWS;
   }
-  p.groups = p.blocks_rb == 1 ? 1024 : 512;
-  p.least = 1;
+  p.groups = 256 * per_unit(dim, p.blocks_rb, dtype == MARS_F32);
   p.nodes = (p.mode == ROWS ? 64 : 16) * p.blocks_rb / group;
   p.bytes = align_up(static_cast<size_t>(p.groups) * 2 * (p.mode == ROWS ? 4 : 1) * piece_bytes(dim, p.blocks_rb));
   return p;
 }
+// Blocks of so few units (as far as the caller says) are not cut: their pieces would have to be joined by a second kernel.
+constexpr int kWholeUnits = 8;
 
-template <int D, int RB, typename T, int MODE> static int launch_attention(const AttnPlan& p, const AttnArgs& a, hipStream_t stream) {
-  if (a.c.log_page >= 5) hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE, true>), dim3(p.groups), dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE, false>), dim3(p.groups), dim3(kThreads), 0, stream, a);
+template <int D, int RB, typename T, int MODE> static int launch_attention(u32 groups, const AttnArgs& a, hipStream_t stream) {
+  if (a.c.log_page >= 5) hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE, true>), dim3(groups), dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE, false>), dim3(groups), dim3(kThreads), 0, stream, a);
   if (hipGetLastError() != hipSuccess) return MARS_ERR_HIP;
-  hipLaunchKernelGGL((merge_kernel<D, RB, T, MODE>), dim3(p.groups - 1, MODE == ROWS ? RB : 1), dim3(kThreads), 0, stream, a, p.groups);
+  if (a.whole) return MARS_OK;
+  hipLaunchKernelGGL((merge_kernel<D, RB, T, MODE>), dim3(groups - 1, MODE == ROWS ? 4 * RB : RB), dim3(kThreads), 0, stream, a, groups);
   return launched();
 }
 
@@ -180,7 +181,7 @@ static bool attention_sizes_ok(int B, int N, int q_heads, int heads, int dim) {
 
 size_t mars_kv_attention_workspace_bytes(int B, int N, int q_heads, int heads, int dim, int dtype) {
   if (!attention_sizes_ok(B, N, q_heads, heads, dim) || !dtype_ok(dtype)) return 0;
-  return attn_plan(B, N, q_heads / heads, dim, dtype).bytes;
+  return attn_plan(N, q_heads / heads, dim, dtype).bytes;
 }
 
 int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs, const mars_kv_rows* q, int dtype, int q_heads,
@@ -193,7 +194,7 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
   if (!dtype_ok(dtype)) return MARS_ERR_DTYPE;
   if (!rows_ok(q, dtype) || !rows_ok(out, dtype) || max_len < 0 || !(scale > 0.0f) || !std::isfinite(scale) || (mask && N > MARS_MAX_NODES))
     return MARS_ERR_ARG;
-  const AttnPlan p = attn_plan(B, N, q_heads / c.heads, cache->dim, dtype);
+  const AttnPlan p = attn_plan(N, q_heads / c.heads, cache->dim, dtype);
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < p.bytes) return MARS_ERR_WORKSPACE;
   AttnArgs a{};
   a.c = c;
@@ -210,16 +211,19 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
   a.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
   a.B = B; a.N = N; a.q_heads = q_heads; a.group = q_heads / c.heads; a.words = (N + 63) / 64;
   a.nodes = p.nodes;
-  a.least = p.least;
-  // the deal counts units in 32 bits
-  const double units = static_cast<double>(B) * c.heads * ((N + p.nodes - 1) / p.nodes) * (((static_cast<long>(c.width) << c.log_page) + N + 3 * kUnit) / kUnit);
+  a.least = 1;
+  const long most_len = static_cast<long>(c.width) << c.log_page, blocks = static_cast<long>(B) * c.heads * ((N + p.nodes - 1) / p.nodes);
+  const double units = static_cast<double>(blocks) * ((most_len + N + 3 * kUnit) / kUnit);  // at most; counted in 32 bits
   if (units > 4.0e9) return MARS_ERR_ARG;
+  a.whole = ((max_len && max_len < most_len ? max_len : most_len) + N + kUnit - 1) / kUnit <= kWholeUnits;
+  const double wanted = a.whole ? (blocks < (1 << 20) ? blocks : 1 << 20) : units < p.groups ? units : p.groups;
+  const u32 groups = (static_cast<u32>(wanted) + 7) / 8 * 8;  // dealt out die by die
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   return by_dim(cache->dim, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    if (dtype == MARS_F32) return p.mode == KEYS ? launch_attention<D, 1, float, KEYS>(p, a, stream) : launch_attention<D, 1, float, ROWS>(p, a, stream);
-    if (p.mode == ROWS) return launch_attention<D, 2, bf16_t, ROWS>(p, a, stream);
-    return p.blocks_rb == 1 ? launch_attention<D, 1, bf16_t, KEYS>(p, a, stream) : launch_attention<D, 2, bf16_t, KEYS>(p, a, stream);
+    if (dtype == MARS_F32) return p.mode == KEYS ? launch_attention<D, 1, float, KEYS>(groups, a, stream) : launch_attention<D, 1, float, ROWS>(groups, a, stream);
+    if (p.mode == ROWS) return launch_attention<D, 2, bf16_t, ROWS>(groups, a, stream);
+    return p.blocks_rb == 1 ? launch_attention<D, 1, bf16_t, KEYS>(groups, a, stream) : launch_attention<D, 2, bf16_t, KEYS>(groups, a, stream);
   });
 }
 

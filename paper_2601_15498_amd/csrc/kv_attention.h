@@ -50,6 +50,7 @@ struct AttnArgs {
   float scale_log2;
   int B, N, q_heads, group, words;
   int nodes;    // of a block of rows
+  bool whole;   // the deal gives out whole blocks
   u32 least;    // units a work-group takes at least
 };
 
@@ -86,7 +87,7 @@ template <int TERMS> __device__ __forceinline__ void split_pair(float a, float b
 // ---------------------------------------------------------------- the deal
 // A request's items are (cache head, block of `nodes` nodes), its units those of its items.  Under a mask a block has all the request's keys.
 // In a chain it has those up to its last node, and blocks are taken in pairs, the last with the first and so on, so that every pair has about
-// the same number of units: `per`, which is rounded up (what is left over of it is idle).
+// the same number of units: `per`, which is rounded up (what is left over of it is idle).  Where whole blocks are given out, one counts as a unit.
 struct Request {
   int n, len, blocks, pairs;  // pairs: of blocks, or blocks
   u32 per;                    // units of a pair, or of a block
@@ -98,9 +99,9 @@ struct Request {
     if (s >= 0) len = min(max(a.c.lens[s], 0), a.c.width << a.c.log_page);
     else n = 0;
     blocks = (n + a.nodes - 1) / a.nodes;
-    const bool paired = !a.mask && blocks > 1;
+    const bool paired = !a.mask && !a.whole && blocks > 1;
     pairs = paired ? (blocks + 1) / 2 : blocks;
-    per = paired ? (2u * len + static_cast<u32>(blocks + 1) * a.nodes + 2 * (kUnit - 1)) / kUnit : static_cast<u32>(len + n + kUnit - 1) / kUnit;
+    per = a.whole ? 1 : paired ? (2u * len + static_cast<u32>(blocks + 1) * a.nodes + 2 * (kUnit - 1)) / kUnit : static_cast<u32>(len + n + kUnit - 1) / kUnit;
   }
   __device__ __forceinline__ u32 units(const AttnArgs& a) const { return static_cast<u32>(a.c.heads) * pairs * per; }
   // Keys that a block's rows see at most.
@@ -543,33 +544,39 @@ __device__ __forceinline__ void attend(const AttnArgs& a, Wave<D, RB, T>& w, con
   }
 }
 
-// Where the results of a lane go: element [f][i] of row rb is channel (4g + i) * D/16 + f.
-template <int D, int RB, typename T>
-__device__ __forceinline__ void write_rows(const AttnArgs& a, int b, int head, int node0, int row0, int rb, int rows, const f32x4 (&o)[D / 16], float m, float l) {
+// Where the results of a lane go: element [f][i] of its row among the 16 from `row0` on is channel (4g + i) * D/16 + f0 + f.
+template <int D, int F, typename T>
+__device__ __forceinline__ void write_part(const AttnArgs& a, int b, int head, int node0, int row0, int rows, int f0, const f32x4 (&o)[F], float m, float l) {
   constexpr int C = D / 16;
   const int lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
-  const int row = row0 + rb * 16 + r;
+  const int row = row0 + r;
   if (row >= rows) return;
   const int in = row / a.group, node = node0 + in, h = head * a.group + row - in * a.group;
   const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
-  T* at = static_cast<T*>(a.out) + b * a.out_request + node * a.out_node + h * a.out_head + g * (4 * C);
+  T* at = static_cast<T*>(a.out) + b * a.out_request + node * a.out_node + h * a.out_head + g * (4 * C) + f0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
+    float x[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) x[f] = o[f][i] * inverse;
     if constexpr (std::is_same<T, float>::value) {
+      if constexpr (F == 1) at[i * C] = x[0];
+      else if constexpr (F == 2) *reinterpret_cast<f32x2*>(at + i * C) = f32x2{x[0], x[1]};
+      else
 #pragma unroll
-      for (int f = 0; f < C; f += 4)
-        *reinterpret_cast<f32x4*>(at + i * C + f) = f32x4{o[f][i] * inverse, o[f + 1][i] * inverse, o[f + 2][i] * inverse, o[f + 3][i] * inverse};
-    } else if constexpr (C >= 8) {
-#pragma unroll
-      for (int f = 0; f < C; f += 8)
-        *reinterpret_cast<u32x4*>(at + i * C + f) =
-            u32x4{round_pair(o[f][i] * inverse, o[f + 1][i] * inverse), round_pair(o[f + 2][i] * inverse, o[f + 3][i] * inverse),
-                  round_pair(o[f + 4][i] * inverse, o[f + 5][i] * inverse), round_pair(o[f + 6][i] * inverse, o[f + 7][i] * inverse)};
+        for (int f = 0; f < F; f += 4) *reinterpret_cast<f32x4*>(at + i * C + f) = f32x4{x[f], x[f + 1], x[f + 2], x[f + 3]};
     } else {
-      *reinterpret_cast<u32x2*>(at + i * C) = u32x2{round_pair(o[0][i] * inverse, o[1][i] * inverse), round_pair(o[2][i] * inverse, o[3][i] * inverse)};
+      if constexpr (F == 1) at[i * C] = static_cast<bf16_t>(round_pair(x[0], 0.0f));
+      else if constexpr (F == 2) *reinterpret_cast<u32*>(at + i * C) = round_pair(x[0], x[1]);
+      else if constexpr (F == 4) *reinterpret_cast<u32x2*>(at + i * C) = u32x2{round_pair(x[0], x[1]), round_pair(x[2], x[3])};
+      else
+#pragma unroll
+        for (int f = 0; f < F; f += 8)
+          *reinterpret_cast<u32x4*>(at + i * C + f) = u32x4{round_pair(x[f], x[f + 1]), round_pair(x[f + 2], x[f + 3]),
+                                                            round_pair(x[f + 4], x[f + 5]), round_pair(x[f + 6], x[f + 7])};
     }
   }
-  if (a.lse && g == 0)
+  if (a.lse && g == 0 && f0 == 0)
     a.lse[(static_cast<size_t>(b) * a.N + node) * a.q_heads + h] =
         l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
@@ -601,16 +608,17 @@ template <typename T, int D> __device__ __forceinline__ void clear_rows(const At
 enum { KEYS = 0, ROWS = 1 };  // what the waves of a work-group divide between them
 template <int MODE, int RB> constexpr int rows_per_block = MODE == KEYS ? 16 * RB : 64 * RB;
 // Work-groups that have to fit a compute unit beside each other: what the compiler may give a wave of registers, and the ring of LDS.
-template <int D, int RB, typename T> constexpr int per_unit = D == 256 ? (RB == 1 && !std::is_same<T, float>::value ? 2 : 1) : std::is_same<T, float>::value ? 2 : RB == 1 ? 3 : 2;
+constexpr int per_unit(int D, int RB, bool f32) { return D == 256 ? (RB == 1 && !f32 ? 2 : 1) : f32 ? 2 : RB == 1 ? 3 : 2; }
+template <int D, int RB, typename T> constexpr int kPerUnit = per_unit(D, RB, std::is_same<T, float>::value);
 constexpr int stages_of(int D, int groups) {  // units in the ring, the one that is worked on among them
   const int n = (160 * 1024 / groups - 1024) / (kWaves * (32 * D + (D <= 128 ? 256 : 512)));
   return n > 4 ? 4 : n;
 }
 
 template <int D, int RB, typename T, int MODE, bool UNIFORM>
-__global__ void __launch_bounds__(kThreads, (per_unit<D, RB, T>)) attention_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kernel(AttnArgs a) {
   using X = Tile<D>;
-  constexpr int NF = D / 16, STAGES = stages_of(D, per_unit<D, RB, T>);
+  constexpr int NF = D / 16, STAGES = stages_of(D, kPerUnit<D, RB, T>);
   static_assert(STAGES >= 2, "a unit in flight while another is worked on");
   constexpr int kJoin = MODE == KEYS ? 2 * RB * NF * 1024 : 0;  // bytes for two waves' results
   constexpr int kRing = STAGES * kWaves * X::kBytes;
@@ -641,8 +649,9 @@ __global__ void __launch_bounds__(kThreads, (per_unit<D, RB, T>)) attention_kern
       u += p.offset;
       continue;
     }
-    const int units = static_cast<int>(min(p.count - p.offset, unit1 - u));
-    const bool whole = static_cast<u32>(units) == p.count;
+    const u32 taken = min(p.count - p.offset, unit1 - u);
+    const bool whole = taken == p.count;
+    const int units = static_cast<int>(a.whole ? p.r.block_units(a, p.block) : taken);
     const int node0 = p.block * a.nodes, rows = min(a.nodes, p.r.n - node0) * a.group, row0 = MODE == ROWS ? wave * 16 * RB : 0;
     const int len = p.r.len, n = p.r.n, end = len + n;
     // no row of this wave sees keys from here on (-1: it has no rows)
@@ -729,7 +738,7 @@ __global__ void __launch_bounds__(kThreads, (per_unit<D, RB, T>)) attention_kern
           f32x4 o[NF];
 #pragma unroll
           for (int f = 0; f < NF; ++f) o[f] = w.o[f][rb];
-          write_rows<D, RB, T>(a, p.b, p.head, node0, row0, rb, rows, o, w.m[rb], w.l[rb]);
+          write_part<D, NF, T>(a, p.b, p.head, node0, row0 + rb * 16, rows, 0, o, w.m[rb], w.l[rb]);
         }
       } else {
         // the first piece of the group's run, or its last one
@@ -746,15 +755,16 @@ __global__ void __launch_bounds__(kThreads, (per_unit<D, RB, T>)) attention_kern
         }
       }
     }
-    u += units;
+    u += taken;
   }
 }
 
 // Joins the pieces of blocks that were dealt to several work-groups: one work-group for every place where the deal cuts one, of which the
-// first of a block takes it; a wave per 16 rows and quarter of the channels.
+// first of a block takes it; a wave per 16 rows and quarter of the result's channels, eight pieces at a time under way (it is the latency of
+// these loads that counts: a piece at a time took 8 us where this takes 4).
 template <int D, int RB, typename T, int MODE>
 __global__ void __launch_bounds__(kThreads) merge_kernel(AttnArgs a, u32 groups) {
-  constexpr int NF = D / 16;
+  constexpr int NF = D / 16, F = NF / 4, AT_ONCE = D == 256 ? 4 : 8;
   Deal deal(a);
   const u32 share = share_of(deal.total, groups, a.least);
   const u32 cut = blockIdx.x + 1;
@@ -766,28 +776,44 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(AttnArgs a, u32 groups)
   if (cut != first + 1) return;                       // an earlier cut's
   const int node0 = p.block * a.nodes, rows = min(a.nodes, p.r.n - node0) * a.group;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 16;
-  constexpr int STRIPS = MODE == ROWS ? 4 * RB : RB;   // of 16 rows
-  for (int strip = blockIdx.y * 4 + wave; strip < STRIPS; strip += gridDim.y * 4) {
-    const int part = MODE == ROWS ? strip / RB : 0, rb = MODE == ROWS ? strip % RB : strip;
-    auto slot = [&](u32 group) {
-      const u32 second = static_cast<unsigned long long>(group) * share >= p.begin ? 0 : 1;
-      return (static_cast<long>(group) * 2 + second) * (MODE == ROWS ? 4 : 1) + part;
-    };
-    float m = kFloor;
-    for (u32 x = first; x <= last; ++x) m = fmaxf(m, Piece<D, RB>(a.partial, slot(x)).reference(rb * 16 + r));
-    float l = 0.0f;
-    f32x4 o[NF];
+  const int strip = blockIdx.y, f0 = wave * F;         // of 16 rows
+  const int part = MODE == ROWS ? strip / RB : 0, rb = MODE == ROWS ? strip % RB : strip;
+  if (part * 16 * RB + rb * 16 >= rows) return;
+  float m = kFloor, l = 0.0f;
+  f32x4 o[F];
 #pragma unroll
-    for (int f = 0; f < NF; ++f) o[f] = f32x4{0, 0, 0, 0};
-    for (u32 x = first; x <= last; ++x) {
-      const Piece<D, RB> piece(a.partial, slot(x));
-      const float weight = __builtin_amdgcn_exp2f(piece.reference(rb * 16 + r) - m);
-      l += piece.sum(rb * 16 + r) * weight;
+  for (int f = 0; f < F; ++f) o[f] = f32x4{0, 0, 0, 0};
+  for (u32 x0 = first; x0 <= last; x0 += AT_ONCE) {
+    float pm[AT_ONCE], pl[AT_ONCE];
+    f32x4 po[AT_ONCE][F];
 #pragma unroll
-      for (int f = 0; f < NF; ++f) o[f] += piece.part(rb, f, lane) * weight;
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const u32 x = min(x0 + i, last);
+      const u32 second = static_cast<unsigned long long>(x) * share >= p.begin ? 0 : 1;
+      const Piece<D, RB> piece(a.partial, (static_cast<long>(x) * 2 + second) * (MODE == ROWS ? 4 : 1) + part);
+      pm[i] = piece.reference(rb * 16 + r);
+      pl[i] = piece.sum(rb * 16 + r);
+#pragma unroll
+      for (int f = 0; f < F; ++f) po[i][f] = piece.part(rb, f0 + f, lane);
     }
-    write_rows<D, RB, T>(a, p.b, p.head, node0, part * 16 * RB, rb, rows, o, m, l);
+    const float before = m;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) m = fmaxf(m, pm[i]);
+    const float shrink = __builtin_amdgcn_exp2f(before - m);
+    l *= shrink;
+#pragma unroll
+    for (int f = 0; f < F; ++f) o[f] *= shrink;
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      if (x0 + i <= last) {
+        const float weight = __builtin_amdgcn_exp2f(pm[i] - m);
+        l += pl[i] * weight;
+#pragma unroll
+        for (int f = 0; f < F; ++f) o[f] += po[i][f] * weight;
+      }
+    }
   }
+  write_part<D, F, T>(a, p.b, p.head, node0, part * 16 * RB + rb * 16, rows, f0, o, m, l);
 }
 
 }  // namespace kv
