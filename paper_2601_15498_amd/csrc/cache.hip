@@ -58,6 +58,8 @@ template <typename F> static int by_type(int dtype, F f) { return dtype == MARS_
 
 static int row_octets(int N) { return (N + 6) / 8 + 1; }  // octets that N positions can touch
 
+constexpr int kCommitGroups = 2048;
+
 // ---------------------------------------------------------------- attention: how the work is laid out
 struct AttnPlan {
   int mode, blocks_rb;  // waves divide keys or rows; blocks of 16 rows per wave
@@ -99,17 +101,13 @@ template <int D, int RB, typename T, int MODE> static int launch_attention(u32 g
   return launched();
 }
 
-static ReserveSpace reserve_space(char* ws, int pages, int B) {
-  ReserveSpace r;
+static ReserveSpace reserve_space(char* ws, int B) {
   const size_t n = align_up(sizeof(int32_t) * B);
-  r.shared = reinterpret_cast<int32_t*>(ws);
-  r.wants = reinterpret_cast<int32_t*>(ws + n);
-  r.begin = reinterpret_cast<int32_t*>(ws + 2 * n);
-  r.copy_src = reinterpret_cast<int32_t*>(ws + 3 * n);
-  r.copy_dst = reinterpret_cast<int32_t*>(ws + 4 * n);
-  r.copies = reinterpret_cast<int32_t*>(ws + 5 * n);
-  r.found = reinterpret_cast<int32_t*>(ws + 5 * n + kAlign);
-  (void)pages;
+  ReserveSpace r;
+  r.copy_src = reinterpret_cast<int32_t*>(ws);
+  r.copy_dst = reinterpret_cast<int32_t*>(ws + n);
+  r.copies = reinterpret_cast<int32_t*>(ws + 2 * n);
+  r.found = reinterpret_cast<int32_t*>(ws + 2 * n + kAlign);
   return r;
 }
 static u32 copy_groups(const Cache& c, long pairs) {
@@ -231,13 +229,17 @@ int mars_kv_commit(const mars_kv_cache* cache, const int32_t* seqs, const int32_
                    int32_t* new_lens, int32_t* status, void* hip_stream) {
   Cache c;
   if (!batch_ok(B, N) || !cache_ok(cache, POOL | TABLE | LENS, &c) || !accept_len || !path_idx || !new_lens) return MARS_ERR_ARG;
-  const long groups = static_cast<long>(B) * c.layers * ((c.heads + 3) / 4);
+  // layers per work-group: so that the chip holds about all of them at once
+  const long quads = static_cast<long>(B) * ((c.heads + 3) / 4);
+  const int per_group = static_cast<int>((quads * c.layers + kCommitGroups - 1) / kCommitGroups);
+  const int layers = per_group < c.layers ? per_group : c.layers;
+  const long groups = quads * ((c.layers + layers - 1) / layers);
   if (groups > 0x7FFFFFFFl) return MARS_ERR_ARG;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   int32_t* apart = new_lens == c.lens ? nullptr : new_lens;
   const int rc = by_dim(cache->dim, [&](auto dim) {
     hipLaunchKernelGGL((commit_kernel<decltype(dim)::value>), dim3(static_cast<u32>(groups)), dim3(256), 0, stream, c, seqs, accept_len, path_idx, B, N,
-                       apart, status);
+                       layers, apart, status);
     return launched();
   });
   if (rc != MARS_OK || apart) return rc;
@@ -247,7 +249,7 @@ int mars_kv_commit(const mars_kv_cache* cache, const int32_t* seqs, const int32_
 
 size_t mars_kv_reserve_workspace_bytes(int pages, int B) {
   if (pages < 1 || pages > (1 << 30) || B < 1 || B > MARS_KV_MAX_REQUESTS) return 0;
-  return 5 * align_up(sizeof(int32_t) * B) + kAlign + align_up(sizeof(int32_t) * pages);
+  return 2 * align_up(sizeof(int32_t) * B) + kAlign + align_up(sizeof(int32_t) * pages);
 }
 
 int mars_kv_reserve(const mars_kv_cache* cache, const int32_t* seqs, const int32_t* n_new, int B, int N, int32_t* status, void* workspace,
@@ -256,7 +258,7 @@ int mars_kv_reserve(const mars_kv_cache* cache, const int32_t* seqs, const int32
   if (!batch_ok(B, N) || !cache_ok(cache, POOL | TABLE | LENS | HELD | REFS, &c)) return MARS_ERR_ARG;
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < mars_kv_reserve_workspace_bytes(c.pages, B))
     return MARS_ERR_WORKSPACE;
-  const ReserveSpace ws = reserve_space(static_cast<char*>(workspace), c.pages, B);
+  const ReserveSpace ws = reserve_space(static_cast<char*>(workspace), B);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kPlanThreads), 0, stream, c, seqs, n_new, B, N, status, ws);
   if (hipGetLastError() != hipSuccess) return MARS_ERR_HIP;

@@ -10,17 +10,13 @@ namespace kv {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
 
-// Workspace of a reserve: per request what it wants, then the pages found and the copies to make.
+// Workspace of a reserve: the pages found, the copies to make.
 struct ReserveSpace {
-  int32_t *shared;  // [B] page in which the request's first new token goes, if that page has tokens already; -1
-  int32_t *wants;   // [B] pages it gets; the copy among them is bit 30
-  int32_t *begin;   // [B] first of them among the found
-  int32_t *found;   // [pages]
+  int32_t* found;                // [pages]
   int32_t *copy_src, *copy_dst;  // [B]
-  int32_t *copies;  // [1]
+  int32_t* copies;               // [1]
 };
-constexpr int kCopyBit = 1 << 30;
-
+constexpr int kCopyBit = 1 << 30;  // of the pages a request wants: the first is to be a copy of the one it shares
 // Sum of v over the threads in front of this one, and over all.
 __device__ __forceinline__ int scan(int v, int* sh, int& total) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
@@ -43,141 +39,150 @@ __device__ __forceinline__ int scan(int v, int* sh, int& total) {
   return front + x - v;
 }
 
-// One work-group: requests' wants, the lowest free pages, the tables.
-// What bounds it: the latency of a few dependent loads and barriers, and of the way through refs to the free pages
-// (4 096 of them per step).
+// One work-group: requests' wants, the lowest free pages, the tables.  What it knows of the requests lies in LDS.
+// What bounds it: the latency of its chain of loads (sequence, length, page, count) and barriers, and the way through refs to the free
+// pages, 16 384 of them per step.
 __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Cache c, const int32_t* __restrict__ seqs, const int32_t* __restrict__ n_new,
                                                                int B, int N, int32_t* __restrict__ status, ReserveSpace ws) {
   __shared__ int sh[kPlanWaves];
-  __shared__ int tile[kPlanThreads];
+  __shared__ __attribute__((aligned(16))) int sh_shared[MARS_KV_MAX_REQUESTS + 3];
+  __shared__ int sh_seq[MARS_KV_MAX_REQUESTS], sh_held[MARS_KV_MAX_REQUESTS], sh_wants[MARS_KV_MAX_REQUESTS], sh_begin[MARS_KV_MAX_REQUESTS];
+  __shared__ uint8_t sh_why[MARS_KV_MAX_REQUESTS];
   const int tid = threadIdx.x, P = 1 << c.log_page;
 
   // what every request needs; the page its first new token goes to
+  bool any = false;  // a page that others hold too
   for (int b = tid; b < B; b += kPlanThreads) {
     const int s = sequence_of(c, seqs, b);
-    int shared = -1, wants = 0, why = MARS_KV_OK;
+    int shared = -1, wants = 0, held = 0, why = MARS_KV_OK;
     if (s < 0) {
       why = MARS_KV_BAD_SEQUENCE;
     } else {
-      const int len = max(c.lens[s], 0), held = min(max(c.held[s], 0), c.width), n = n_new ? min(max(n_new[b], 0), N) : N;
+      const int len = max(c.lens[s], 0), n = n_new ? min(max(n_new[b], 0), N) : N;
+      held = min(max(c.held[s], 0), c.width);
       const long need = (static_cast<long>(len) + n + P - 1) >> c.log_page;
       if (need > c.width) {
         why = MARS_KV_TOO_LONG;
       } else {
         wants = max(static_cast<int>(need) - held, 0);
-        const int at = len >> c.log_page;
-        if ((len & (P - 1)) && n > 0 && at < held) shared = page_of(c, s, len);
+        if ((len & (P - 1)) && n > 0 && len >> c.log_page < held) shared = page_of(c, s, len);
       }
     }
-    ws.shared[b] = shared;
-    ws.wants[b] = wants;
-    if (status) status[b] = why;
+    sh_seq[b] = s;
+    sh_held[b] = held;
+    sh_shared[b] = shared;
+    sh_wants[b] = wants;
+    sh_why[b] = static_cast<uint8_t>(why);
+    any |= shared >= 0 && c.refs[shared] > 1;
   }
-  __syncthreads();
-
+  if (tid < 3) sh_shared[B + tid] = -1;
   // a page that others hold too is copied, unless this is the last of its holders and all of them are here
-  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
-    const int b = b0 + tid;
-    const int mine = b < B ? ws.shared[b] : -1;
-    const int holders = mine >= 0 ? c.refs[mine] : 0;
-    int here = 0, later = 0;
-    if (__syncthreads_or(holders > 1)) {
-      for (int t0 = 0; t0 < B; t0 += kPlanThreads) {
-        __syncthreads();
-        tile[tid] = t0 + tid < B ? ws.shared[t0 + tid] : -1;
-        __syncthreads();
-        if (holders > 1) {
-          const int m = min(kPlanThreads, B - t0);
-          for (int i = 0; i < m; ++i) {
-            const bool same = tile[i] == mine;
-            here += same;
-            later += same && t0 + i > b;
-          }
-        }
+  if (__syncthreads_or(any)) {
+    for (int b = tid; b < B; b += kPlanThreads) {
+      const int mine = sh_shared[b], holders = mine >= 0 ? c.refs[mine] : 0;
+      if (holders <= 1) continue;
+      int here = 0, later = 0;
+      for (int i = 0; i < B; i += 4) {
+        const int4 x = *reinterpret_cast<const int4*>(sh_shared + i);
+        const bool e0 = x.x == mine, e1 = x.y == mine, e2 = x.z == mine, e3 = x.w == mine;
+        here += e0 + e1 + e2 + e3;
+        later += (e0 && i > b) + (e1 && i + 1 > b) + (e2 && i + 2 > b) + (e3 && i + 3 > b);
       }
+      if (later > 0 || holders > here) sh_wants[b] = (sh_wants[b] + 1) | kCopyBit;
     }
-    if (holders > 1 && (later > 0 || holders > here)) ws.wants[b] = (ws.wants[b] + 1) | kCopyBit;
+    __syncthreads();
   }
-  __syncthreads();
 
   // in order of the requests
   long demand = 0;
   for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
     const int b = b0 + tid;
     int total;
-    const int want = b < B ? ws.wants[b] & ~kCopyBit : 0;
-    const int before = scan(want, sh, total);
-    if (b < B) ws.begin[b] = static_cast<int>(min(demand + before, 0x3FFFFFFFl));
+    const int before = scan(b < B ? sh_wants[b] & ~kCopyBit : 0, sh, total);
+    if (b < B) sh_begin[b] = static_cast<int>(min(demand + before, 0x3FFFFFFFl));
     demand += total;
   }
 
   // the lowest free pages, as many as are wanted
   const int most = static_cast<int>(min(demand, static_cast<long>(c.pages)));
   int have = 0;
-  for (int p0 = 0; p0 < c.pages && have < most; p0 += kPlanThreads * 4) {
-    const int p = p0 + tid * 4;
-    int free[4];
+  for (int p0 = 0; p0 < c.pages && have < most; p0 += kPlanThreads * 16) {
+    const int p = p0 + tid * 16;
+    u32 free = 0;
+    if (p + 16 <= c.pages && reinterpret_cast<uintptr_t>(c.refs) % 16 == 0) {
+      int4 x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) free[i] = p + i < c.pages && c.refs[p + i] == 0;
+      for (int i = 0; i < 4; ++i) x[i] = reinterpret_cast<const int4*>(c.refs + p)[i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        free |= ((x[i].x == 0) | (x[i].y == 0) << 1 | (x[i].z == 0) << 2 | (x[i].w == 0) << 3) << (4 * i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (p + i < c.pages && c.refs[p + i] == 0) free |= 1u << i;
+    }
     int total;
-    int at = have + scan(free[0] + free[1] + free[2] + free[3], sh, total);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (free[i] && at < most) ws.found[at] = p + i;
-      at += free[i];
+    int at = have + scan(__popc(free), sh, total);
+    while (free && at < most) {
+      ws.found[at++] = p + __ffs(free) - 1;
+      free &= free - 1;
     }
     have += total;
   }
   have = min(have, most);
   __syncthreads();
 
-  // the tables: a wave per request.  (A request that does not get all it wants gets nothing; begin only grows, so those behind
-  // it that want any get nothing either.)
+  // A request that does not get all it wants gets nothing; begin only grows, so those behind it that want any get nothing either.
   int copies = 0;  // those in front, the same in all threads
   for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
     const int b = b0 + tid;
-    const int want = b < B ? ws.wants[b] : 0;
-    const bool fits = b < B && ws.begin[b] + (want & ~kCopyBit) <= have;
-    const bool copy = fits && (want & kCopyBit);
+    const int want = b < B ? sh_wants[b] & ~kCopyBit : 0;
+    const bool fits = b < B && sh_begin[b] + want <= have, copy = fits && (sh_wants[b] & kCopyBit);
     int total;
     const int rank = copies + scan(copy, sh, total);
-    if (copy) {
-      ws.copy_src[rank] = ws.shared[b];
-      ws.copy_dst[rank] = ws.found[ws.begin[b]];
-    }
-    if (b < B && !fits && (want & ~kCopyBit) && status) status[b] = MARS_KV_NO_PAGES;
     copies += total;
+    if (b < B && want) {
+      if (!fits) {
+        sh_why[b] = MARS_KV_NO_PAGES;
+      } else {
+        const int s = sh_seq[b];
+        if (copy) {
+          const int page = ws.found[sh_begin[b]];
+          ws.copy_src[rank] = sh_shared[b];
+          ws.copy_dst[rank] = page;
+          atomicSub(&c.refs[sh_shared[b]], 1);
+          c.refs[page] = 1;
+          c.page_table[static_cast<size_t>(s) * c.width + (max(c.lens[s], 0) >> c.log_page)] = page;
+        }
+        c.held[s] = sh_held[b] + want - copy;
+      }
+    }
   }
   if (tid == 0) *ws.copies = copies;
-  const int lane = tid % kWave;
-  for (int b = tid / kWave; b < B; b += kPlanWaves) {
-    const int want = ws.wants[b] & ~kCopyBit, begin = ws.begin[b];
-    const bool copy = (ws.wants[b] & kCopyBit) != 0;
-    if (want == 0 || begin + want > have) continue;
-    const int s = sequence_of(c, seqs, b);
-    if (s < 0) continue;
-    const int held = min(max(c.held[s], 0), c.width), fresh = want - copy;
-    int32_t* row = c.page_table + static_cast<size_t>(s) * c.width;
-    if (copy && lane == 0) {
-      const int page = ws.found[begin];
-      atomicSub(&c.refs[ws.shared[b]], 1);
-      c.refs[page] = 1;
-      row[max(c.lens[s], 0) >> c.log_page] = page;
+  // the pages that are added: a thread per page, which looks its request up
+  for (int k = tid; k < have; k += kPlanThreads) {
+    int lo = 0, hi = B - 1;  // the last request that begins at k or before; those that want none come before it or begin later
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (sh_begin[mid] <= k) lo = mid;
+      else hi = mid - 1;
     }
-    for (int i = lane; i < fresh; i += kWave) {
-      const int page = ws.found[begin + copy + i];
-      c.refs[page] = 1;
-      row[held + i] = page;
-    }
-    if (lane == 0) c.held[s] = held + fresh;
+    const int want = sh_wants[lo] & ~kCopyBit, copy = (sh_wants[lo] & kCopyBit) != 0, i = k - sh_begin[lo] - copy;
+    if (i < 0 || k >= sh_begin[lo] + want || sh_begin[lo] + want > have) continue;  // (the copy; pages that nobody gets)
+    const int page = ws.found[k];
+    c.refs[page] = 1;
+    c.page_table[static_cast<size_t>(sh_seq[lo]) * c.width + sh_held[lo] + i] = page;
   }
-  // the last holder of a page keeps it only if the others got their copies (the counts are read past the first cache, where the
-  // subtractions above were made)
+  // The last holder of a page keeps it only if the others got their copies (the counts are read past the first cache, where the
+  // subtractions above were made).
   __syncthreads();
-  for (int b = tid; status && b < B; b += kPlanThreads)
-    if (ws.shared[b] >= 0 && !(ws.wants[b] & kCopyBit) && status[b] == MARS_KV_OK &&
-        __hip_atomic_load(&c.refs[ws.shared[b]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 1)
-      status[b] = MARS_KV_NO_PAGES;
+  for (int b = tid; status && b < B; b += kPlanThreads) {
+    int why = sh_why[b];
+    if (sh_shared[b] >= 0 && !(sh_wants[b] & kCopyBit) && why == MARS_KV_OK &&
+        __hip_atomic_load(&c.refs[sh_shared[b]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 1)
+      why = MARS_KV_NO_PAGES;
+    status[b] = why;
+  }
 }
 
 // A work-group per pair.

@@ -189,23 +189,26 @@ __device__ __forceinline__ Path check_path(const Cache& c, const int32_t* seqs, 
   if (p.status != MARS_KV_OK) p.n = 0;
   return p;
 }
-// Where piece `lane` of the token at page offset t lies, and whether it is a dword or a byte.
-template <int D> __device__ __forceinline__ u32 piece_at(u32 log_page, u32 t, int piece) {
-  constexpr int W = D / 8, S = D / 32;
-  if (piece < W) return Place<D>::key(t) + piece * 4;
-  if (piece < 2 * W) return Place<D>::value(log_page, t) + (piece - W) * 32;
-  if (piece < 2 * W + S) return Place<D>::key_scale(log_page, t) + (piece - 2 * W);
-  return Place<D>::value_scale(log_page, t) + (piece - 2 * W - S) * 8;
+// Where dword `i` of a token's codes (keys', then values'), and byte `i` of its scales, lie in a head's part of its page.
+template <int D> __device__ __forceinline__ u32 dword_at(u32 log_page, u32 t, int i) {
+  return i < D / 8 ? Place<D>::key(t) + i * 4 : Place<D>::value(log_page, t) + (i - D / 8) * 32;
 }
+template <int D> __device__ __forceinline__ u32 scale_byte_at(u32 log_page, u32 t, int i) {
+  return i < D / 32 ? Place<D>::key_scale(log_page, t) + i : Place<D>::value_scale(log_page, t) + (i - D / 32) * 8;
+}
+// The path is looked at once for `per_group` layers: a wave's chain of loads (length, path, pages) costs as much as a dozen rows, and with a work-group per layer
+// 256 paths in 32 layers took 8 rounds of it (67 us).
 template <int D>
 __global__ void __launch_bounds__(256) commit_kernel(Cache c, const int32_t* __restrict__ seqs, const int32_t* __restrict__ accept_len,
-                                                     const int32_t* __restrict__ path_idx, int B, int N, int32_t* __restrict__ new_lens,
-                                                     int32_t* __restrict__ status) {
-  constexpr int W = D / 8, S = D / 32, PIECES = 2 * W + 2 * S, BATCH = 8;
+                                                     const int32_t* __restrict__ path_idx, int B, int N, int per_group,
+                                                     int32_t* __restrict__ new_lens, int32_t* __restrict__ status) {
+  constexpr int BATCH = 8, DEEP = 4;               // rows, and layers of them, on their way at a time
+  constexpr int WORDS = D / 4, BYTES = D / 16;     // of a row
+  constexpr int WORD_OPS = BATCH * WORDS / kWave, BYTE_OPS = (BATCH * BYTES + kWave - 1) / kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int per_layer = (c.heads + 3) / 4;
-  const int b = blockIdx.x / (c.layers * per_layer), rest = blockIdx.x % (c.layers * per_layer);
-  const int layer = rest / per_layer, h = rest % per_layer * 4 + wave;
+  const int quads = (c.heads + 3) / 4, parts = (c.layers + per_group - 1) / per_group;
+  const int b = blockIdx.x / (parts * quads), rest = blockIdx.x % (parts * quads);
+  const int layer0 = rest / quads * per_group, layer1 = min(layer0 + per_group, c.layers), h = rest % quads * 4 + wave;
   const Path p = check_path(c, seqs, accept_len, path_idx, b, N);
   if (rest == 0 && threadIdx.x == 0) {
     report(status, b, p.status);
@@ -213,41 +216,67 @@ __global__ void __launch_bounds__(256) commit_kernel(Cache c, const int32_t* __r
   }
   if (h >= c.heads) return;
   const int32_t* path = path_idx + static_cast<size_t>(b) * N;
-  const size_t layer_offset = static_cast<size_t>(layer) * c.layer_bytes;
   const u32 in_page = (1u << c.log_page) - 1;
   for (int i0 = 0; i0 < p.n; i0 += BATCH) {
-    const int m = min(BATCH, p.n - i0);
-    // lane i < 8: source of row i0 + i, lane 8 + i: its target
-    int node = 0, page = -1;
+    // lane i < 8: source of row i0 + i, lane 8 + i: its target; -1: no row, or it stays where it is (a chain's)
+    int at = -1, page = -1;
     const int i = i0 + lane % BATCH;
     if (lane < 2 * BATCH && i < p.n) {
-      node = path[i];
-      const int at = p.len + (lane < BATCH ? node : 1 + i);
-      page = page_of(c, p.seq, at);
-      node = at;
+      const int node = path[i];
+      if (node != 1 + i) {
+        at = p.len + (lane < BATCH ? node : 1 + i);
+        page = page_of(c, p.seq, at);
+      }
+    }
+    // the rows that move, beside each other
+    const u32 moves = static_cast<u32>(__ballot(lane < BATCH && page >= 0));
+    if (!moves) continue;
+    const int rows = __popc(moves);
+    auto place = [&](int q, bool source, auto where) -> long {  // offset of the q-th row's piece; -1: no such row
+      u32 rest = moves;
+      for (int k = 0; k < BATCH - 1; ++k)
+        if (k < q) rest &= rest - 1;
+      const int j = (q < rows ? __ffs(rest) - 1 : 0) + (source ? 0 : BATCH);
+      const u32 of = __shfl(page, j), t = __shfl(at, j);  // (by all lanes: these are the ones that are read)
+      return q < rows ? static_cast<long>(of) * c.page_bytes + static_cast<long>(h) * c.blk + where(t & in_page) : -1;
+    };
+    long word_from[WORD_OPS], word_to[WORD_OPS], byte_from[BYTE_OPS], byte_to[BYTE_OPS];
+#pragma unroll
+    for (int o = 0; o < WORD_OPS; ++o) {
+      const int piece = o * kWave + lane, q = piece / WORDS;
+      auto where = [&](u32 t) { return dword_at<D>(c.log_page, t, piece % WORDS); };
+      word_from[o] = place(q, true, where);
+      word_to[o] = place(q, false, where);
     }
 #pragma unroll
-    for (int r = 0; r < (PIECES + kWave - 1) / kWave; ++r) {
-      const int piece = r * kWave + lane;
-      const bool dword = piece < 2 * W, live = piece < PIECES;
-      u32 x[BATCH];
+    for (int o = 0; o < BYTE_OPS; ++o) {
+      const int piece = o * kWave + lane, q = piece / BYTES;
+      auto where = [&](u32 t) { return scale_byte_at<D>(c.log_page, t, piece % BYTES); };
+      byte_from[o] = place(q, true, where);
+      byte_to[o] = place(q, false, where);
+    }
+    for (int layer = layer0; layer < layer1; layer += DEEP) {
+      uint8_t* const base = c.pool + static_cast<size_t>(layer) * c.layer_bytes;
+      u32 x[DEEP][WORD_OPS], y[DEEP][BYTE_OPS];
 #pragma unroll
-      for (int j = 0; j < BATCH; ++j) {
-        x[j] = 0;
-        const int sp = __builtin_amdgcn_readlane(page, j), st = __builtin_amdgcn_readlane(node, j);
-        if (j < m && sp >= 0 && live && st != __builtin_amdgcn_readlane(node, BATCH + j)) {  // (a chain's rows stay)
-          const uint8_t* from = head_of(c, layer_offset, sp, h) + piece_at<D>(c.log_page, st & in_page, piece);
-          x[j] = dword ? *reinterpret_cast<const u32*>(from) : *from;
-        }
+      for (int d = 0; d < DEEP; ++d) {
+        if (layer + d >= layer1) break;
+#pragma unroll
+        for (int o = 0; o < WORD_OPS; ++o)
+          if (o * kWave / WORDS < rows && word_from[o] >= 0) x[d][o] = *reinterpret_cast<const u32*>(base + d * c.layer_bytes + word_from[o]);
+#pragma unroll
+        for (int o = 0; o < BYTE_OPS; ++o)
+          if (byte_from[o] >= 0) y[d][o] = base[d * c.layer_bytes + byte_from[o]];
       }
 #pragma unroll
-      for (int j = 0; j < BATCH; ++j) {
-        const int tp = __builtin_amdgcn_readlane(page, BATCH + j), tt = __builtin_amdgcn_readlane(node, BATCH + j);
-        if (j < m && tp >= 0 && live && tt != __builtin_amdgcn_readlane(node, j)) {
-          uint8_t* to = head_of(c, layer_offset, tp, h) + piece_at<D>(c.log_page, tt & in_page, piece);
-          if (dword) *reinterpret_cast<u32*>(to) = x[j];
-          else *to = static_cast<uint8_t>(x[j]);
-        }
+      for (int d = 0; d < DEEP; ++d) {
+        if (layer + d >= layer1) break;
+#pragma unroll
+        for (int o = 0; o < WORD_OPS; ++o)
+          if (o * kWave / WORDS < rows && word_to[o] >= 0) *reinterpret_cast<u32*>(base + d * c.layer_bytes + word_to[o]) = x[d][o];
+#pragma unroll
+        for (int o = 0; o < BYTE_OPS; ++o)
+          if (byte_to[o] >= 0) base[d * c.layer_bytes + byte_to[o]] = static_cast<uint8_t>(y[d][o]);
       }
     }
   }
