@@ -331,12 +331,10 @@ template <int D, bool UNIFORM> struct Fetch {
     return bad;
   }
 };
-// What a lane has of a tile, in registers.
-template <int D> struct Share {
-  static constexpr int S = D / 32, VW = Tile<D>::VW;
-  u32 k[2][S], ks[2], v[VW];
-  u32x2 vs;
-  __device__ __forceinline__ explicit Share(const uint8_t* tile) {
+// What a lane has of a tile, in registers: sixteen keys' quarter twice, and eight keys' values.
+template <int D> struct Keys {
+  u32 k[2][D / 32], ks[2];
+  __device__ __forceinline__ explicit Keys(const uint8_t* tile) {
     using X = Tile<D>;
     const u32 lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
     const uint8_t* scales = tile + 2 * X::kCodes;
@@ -358,49 +356,181 @@ template <int D> struct Share {
         else ks[b] = scales[t * 8 + g] | static_cast<u32>(scales[t * 8 + 4 + g]) << 8;
       }
     }
+  }
+};
+// Two keys' values of the same channel beside each other: the low halves of two conversions, or the high ones.
+__device__ __forceinline__ u32 low_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+template <int D> struct Values {
+  u32 v[Tile<D>::VW];
+  u32x2 vs;
+  __device__ __forceinline__ explicit Values(const uint8_t* tile) {
+    using X = Tile<D>;
+    const u32 lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
 #pragma unroll
-    for (int i = 0; i < VW / 4; ++i) {
+    for (int i = 0; i < X::VW / 4; ++i) {
       const u32 c = D == 64 ? r >> 1 : D == 128 ? r : 2 * r + (i >> 1);
       const u32x4 w = *reinterpret_cast<const u32x4*>(tile + X::kCodes + X::value_slot(g, c, i & 1) * 16);
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[4 * i + j] = w[j];
     }
-    vs = *reinterpret_cast<const u32x2*>(scales + (D <= 128 ? 128 : 256) + g * (D / 4) + (r * (D / 16)) / 32 * 8);
+    vs = *reinterpret_cast<const u32x2*>(tile + 2 * X::kCodes + (D <= 128 ? 128 : 256) + g * (D / 4) + (r * (D / 16)) / 32 * 8);
+  }
+  // Of the lane's eight keys only the first `there` count: past the end of the sequence memory holds anything, and 0 times that has to be 0.
+  __device__ __forceinline__ void cut(int there) {
+    vs[0] = there >= 4 ? vs[0] : there <= 0 ? 0 : vs[0] & ((1u << (8 * there)) - 1);
+    vs[1] = there >= 8 ? vs[1] : there <= 4 ? 0 : vs[1] & ((1u << (8 * (there - 4))) - 1);
+  }
+  // f(n, fragment): operand n of the second product, channels c D/16 + n of lane column c, for all n.
+  template <typename F> __device__ __forceinline__ void each(F f) const {
+    const u32 scale[8] = {scale_at<0>(vs[0]), scale_at<1>(vs[0]), scale_at<2>(vs[0]), scale_at<3>(vs[0]),
+                          scale_at<0>(vs[1]), scale_at<1>(vs[1]), scale_at<2>(vs[1]), scale_at<3>(vs[1])};
+    auto pair = [&](auto byte, int n, const u32* words, u32 shift) {  // channels 2 byte, 2 byte + 1 of a dword column
+      constexpr int BYTE = decltype(byte)::value;
+      u32 y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = decode<BYTE>(words[j] >> shift, scale[j]);
+      f(n, as_bf16x8(low_halves(y[0], y[1]), low_halves(y[2], y[3]), low_halves(y[4], y[5]), low_halves(y[6], y[7])));
+      f(n + 1, as_bf16x8(high_halves(y[0], y[1]), high_halves(y[2], y[3]), high_halves(y[4], y[5]), high_halves(y[6], y[7])));
+    };
+    if constexpr (D == 64) {
+      const u32 shift = (threadIdx.x & 1) * 16;
+      pair(std::integral_constant<int, 0>{}, 0, v, shift);
+      pair(std::integral_constant<int, 1>{}, 2, v, shift);
+    } else {
+#pragma unroll
+      for (int h = 0; h < D / 128; ++h) {
+        pair(std::integral_constant<int, 0>{}, 8 * h, v + 8 * h, 0);
+        pair(std::integral_constant<int, 1>{}, 8 * h + 2, v + 8 * h, 0);
+        pair(std::integral_constant<int, 2>{}, 8 * h + 4, v + 8 * h, 0);
+        pair(std::integral_constant<int, 3>{}, 8 * h + 6, v + 8 * h, 0);
+      }
+    }
   }
 };
 
 // ---------------------------------------------------------------- a wave's rows
-// Channels of the queries (and keys) that lane group g takes in step s: eight from here on.
-template <int D> __device__ __forceinline__ int channel(int g, int s) { return D == 64 ? g * 16 + s * 8 : s / 4 * 128 + g * 32 + s % 4 * 8; }
+// The queries as the first product's second operand.  Three forms:
+//   bf16 rows, D >= 128 (CODES): the keys' codes and scales go into the product as they are (4 bits by 8 bits, a scale per 32 channels), 128 channels at a time;
+//     the queries go in as two 8-bit terms of four significant bits each, which is all that a bf16 number has, with one scale per row: what is lost of a
+//     channel is below 2^-22 of the row's largest.  (The keys converted to bf16 instead: a third of the vector instructions that do not depend on the number of rows.)
+//   bf16 rows, D = 64: keys converted to bf16, 32 channels at a time.
+//   fp32 rows: the same with three bf16 terms.
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+template <int D, typename T> constexpr bool kCodes = D >= 128 && !std::is_same<T, float>::value;
+
+template <int D, int RB, typename T, bool CODES> struct Queries;
+template <int D, int RB, typename T> struct Queries<D, RB, T, false> {
+  static constexpr int S = D / 32, TERMS = std::is_same<T, float>::value ? 3 : 1;
+  bf16x8 q[TERMS][RB][S];
+  // Channels that lane group g takes in step s: eight from here on.
+  __device__ static __forceinline__ int channel(int g, int s) { return D == 64 ? g * 16 + s * 8 : s / 4 * 128 + g * 32 + s % 4 * 8; }
+  __device__ __forceinline__ void load(int rb, const T* row, bool live) {
+    const int g = threadIdx.x % kWave / 16;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      u32 t[4][TERMS];
+      const Eight e = load_eight(row + channel(g, s));
+#pragma unroll
+      for (int p = 0; p < 4; ++p) split_pair<TERMS>(live ? e.x[2 * p] : 0.0f, live ? e.x[2 * p + 1] : 0.0f, t[p]);
+#pragma unroll
+      for (int k = 0; k < TERMS; ++k) q[k][rb][s] = as_bf16x8(t[0][k], t[1][k], t[2][k], t[3][k]);
+    }
+  }
+  __device__ __forceinline__ void scores(const Keys<D>& x, f32x4 (&sc)[2][RB]) const {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) sc[b][rb] = f32x4{0, 0, 0, 0};
+      const u32 s0 = scale_at<0>(x.ks[b]), s1 = D == 256 ? scale_at<1>(x.ks[b]) : s0;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const u32 scale = s < 4 ? s0 : s1;
+        const bf16x8 k = as_bf16x8(decode<0>(x.k[b][s], scale), decode<1>(x.k[b][s], scale), decode<2>(x.k[b][s], scale), decode<3>(x.k[b][s], scale));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+          for (int t = TERMS - 1; t >= 0; --t) sc[b][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[t][rb][s], sc[b][rb], 0, 0, 0);
+      }
+    }
+  }
+};
+template <int D, int RB, typename T> struct Queries<D, RB, T, true> {
+  static constexpr int H = D / 128;
+  i32x8 q[2][RB][H];
+  int scale[2][RB];  // of the row's two terms, as bytes like the keys'
+  __device__ __forceinline__ void load(int rb, const T* row, bool live) {
+    // The 8-bit operand's lane group g has channels 16 g .. + 15 and 64 + 16 g .. + 15 of each 128.
+    const int g = threadIdx.x % kWave / 16;
+    Eight e[H][4];
+    u32 top = 0;
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        e[h][i] = load_eight(row + h * 128 + i / 2 * 64 + g * 16 + i % 2 * 8);
+        top = max(top, top_bits(e[h][i]));
+      }
+    top = live ? top : 0;
+    top = max(top, static_cast<u32>(__shfl_xor(static_cast<int>(top), 16)));
+    top = max(top, static_cast<u32>(__shfl_xor(static_cast<int>(top), 32)));
+    // The largest is 128 to 256 of the first term's steps; the second's are 32 times finer (what the first leaves is at most 8 of its own).
+    const u32 exponent = max(top >> 23, 13u);
+    const bool bad = top >= 0x7F800000u;  // a query that is not finite: its scores are NaN
+    scale[0][rb] = bad ? 255 : static_cast<int>(exponent - 7);
+    scale[1][rb] = bad ? 255 : static_cast<int>(exponent - 12);
+    const float up = live ? __uint_as_float((261 - exponent) << 23) : 0.0f;  // 2^(7 - (exponent - 127))
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float x0 = e[h][i].x[4 * j] * up, x1 = e[h][i].x[4 * j + 1] * up, x2 = e[h][i].x[4 * j + 2] * up, x3 = e[h][i].x[4 * j + 3] * up;
+          int first = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, 0, false);
+          first = __builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, first, true);
+          int second = __builtin_amdgcn_cvt_pk_fp8_f32((x0 - __builtin_amdgcn_cvt_f32_fp8(first, 0)) * 32.0f, (x1 - __builtin_amdgcn_cvt_f32_fp8(first, 1)) * 32.0f, 0, false);
+          second = __builtin_amdgcn_cvt_pk_fp8_f32((x2 - __builtin_amdgcn_cvt_f32_fp8(first, 2)) * 32.0f, (x3 - __builtin_amdgcn_cvt_f32_fp8(first, 3)) * 32.0f, second, true);
+          q[0][rb][h][2 * i + j] = first;
+          q[1][rb][h][2 * i + j] = second;
+        }
+  }
+  template <int H0> __device__ __forceinline__ f32x4 step(const Keys<D>& x, int b, int rb, f32x4 sc) const {
+    const i32x8 k = {static_cast<int>(x.k[b][4 * H0]), static_cast<int>(x.k[b][4 * H0 + 1]), static_cast<int>(x.k[b][4 * H0 + 2]), static_cast<int>(x.k[b][4 * H0 + 3]), 0, 0, 0, 0};
+    const int ks = static_cast<int>(x.ks[b]);
+    sc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q[1][rb][H0], sc, 4, 0, H0, ks, 0, scale[1][rb]);  // (4: codes of 4 bits, 0: of 8)
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q[0][rb][H0], sc, 4, 0, H0, ks, 0, scale[0][rb]);
+  }
+  __device__ __forceinline__ void scores(const Keys<D>& x, f32x4 (&sc)[2][RB]) const {
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        sc[b][rb] = step<0>(x, b, rb, f32x4{0, 0, 0, 0});
+        if constexpr (H == 2) sc[b][rb] = step<1>(x, b, rb, sc[b][rb]);
+      }
+  }
+};
 
 template <int D, int RB, typename T> struct Wave {
-  static constexpr int S = D / 32;              // steps of 32 channels
   static constexpr int NF = D / 16;             // blocks of 16 channels of the result
   static constexpr int TERMS = std::is_same<T, float>::value ? 3 : 1;
-  bf16x8 q[TERMS][RB][S];
+  Queries<D, RB, T, kCodes<D, T>> q;
   f32x4 o[NF][RB];
   float m[RB], l[RB];
   int node[RB];                                 // of this lane's rows; < 0: no row
 
   // Rows row0 .. of the block of nodes from node0 on, which has `rows`.
   __device__ __forceinline__ void start(const AttnArgs& a, int b, int head, int node0, int row0, int rows) {
-    const int lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
+    const int r = threadIdx.x % 16;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const int row = row0 + rb * 16 + r;
       const bool live = row < rows;
       const int in = live ? row / a.group : 0, h = live ? row - in * a.group : 0;
       node[rb] = live ? node0 + in : -1;
-      const T* at = static_cast<const T*>(a.q) + b * a.q_request + static_cast<long>(node0 + in) * a.q_node + static_cast<long>(head * a.group + h) * a.q_head;
-#pragma unroll
-      for (int s = 0; s < S; ++s) {
-        u32 t[4][TERMS];
-        const Eight e = load_eight(at + channel<D>(g, s));
-#pragma unroll
-        for (int p = 0; p < 4; ++p) split_pair<TERMS>(live ? e.x[2 * p] : 0.0f, live ? e.x[2 * p + 1] : 0.0f, t[p]);
-#pragma unroll
-        for (int k = 0; k < TERMS; ++k) q[k][rb][s] = as_bf16x8(t[0][k], t[1][k], t[2][k], t[3][k]);
-      }
+      q.load(rb, static_cast<const T*>(a.q) + b * a.q_request + static_cast<long>(node0 + in) * a.q_node + static_cast<long>(head * a.group + h) * a.q_head, live);
       m[rb] = kFloor;
       l[rb] = 0.0f;
 #pragma unroll
@@ -408,10 +538,6 @@ template <int D, int RB, typename T> struct Wave {
     }
   }
 };
-
-// Two keys' values of the same channel beside each other: the low halves of two conversions, or the high ones.
-__device__ __forceinline__ u32 low_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
-__device__ __forceinline__ u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
 // Which of the keys first .. first + 7 (numbered from the first node on; committed ones are < 0) row `node` of n nodes sees.
 __device__ __forceinline__ u32 seen(const AttnArgs& a, int b, int node, int n, int first) {
@@ -430,33 +556,21 @@ __device__ __forceinline__ u32 seen(const AttnArgs& a, int b, int node, int n, i
   return bits & (k >= 8 ? 0xFFu : k <= 0 ? 0u : (1u << k) - 1);
 }
 
+// Probabilities of a tile's keys as the second product's second operand: TERMS bf16 terms each.
+template <int D, int RB, typename T> struct Weights { u32 p[Wave<D, RB, T>::TERMS][RB][4]; };
+
 // One tile.  `plain` (the same for the wave): every row sees all of it, and all of it is there.  Otherwise: request b has n nodes behind
 // `len` tokens, the tile begins at t0; `poison`: the lane's octet has no page.
 template <int D, int RB, typename T>
-__device__ __forceinline__ void attend(const AttnArgs& a, Wave<D, RB, T>& w, const Share<D>& x, bool plain, int b, int len, int n, int t0, bool poison) {
+__device__ __forceinline__ void weigh(const AttnArgs& a, Wave<D, RB, T>& w, const Keys<D>& x, bool plain, int b, int len, int n, int t0, bool poison,
+                                      Weights<D, RB, T>& y) {
+  constexpr int NF = D / 16, TERMS = Wave<D, RB, T>::TERMS;
   const float c = a.scale_log2;
-  constexpr int S = D / 32, NF = D / 16, TERMS = Wave<D, RB, T>::TERMS;
-  const int lane = threadIdx.x % kWave, r = lane % 16;
   f32x4 sc[2][RB];
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) sc[b][rb] = f32x4{0, 0, 0, 0};
-    const u32 s0 = scale_at<0>(x.ks[b]), s1 = D == 256 ? scale_at<1>(x.ks[b]) : s0;
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const u32 scale = s < 4 ? s0 : s1;
-      const bf16x8 k = as_bf16x8(decode<0>(x.k[b][s], scale), decode<1>(x.k[b][s], scale), decode<2>(x.k[b][s], scale), decode<3>(x.k[b][s], scale));
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-        for (int t = TERMS - 1; t >= 0; --t) sc[b][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, w.q[t][rb][s], sc[b][rb], 0, 0, 0);
-    }
-  }
+  w.q.scores(x, sc);
   __builtin_amdgcn_sched_barrier(0);  // (the values' conversions would be brought up to here, and their results kept)
-  u32 vs0 = x.vs[0], vs1 = x.vs[1];  // scales of the eight keys
   if (!plain) {
-    const int first = t0 + lane / 16 * 8 - len;
+    const int first = t0 + static_cast<int>(threadIdx.x % kWave / 16) * 8 - len;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const u32 sees = w.node[rb] < 0 ? 0u : seen(a, b, w.node[rb], n, first);
@@ -468,10 +582,6 @@ __device__ __forceinline__ void attend(const AttnArgs& a, Wave<D, RB, T>& w, con
           sc[k][rb][i] = sees >> (4 * k + i) & 1 ? s : -__builtin_inff();
         }
     }
-    // past the end of the sequence memory holds anything, and 0 times that has to be 0
-    const int there = n - first;  // of the lane's eight keys
-    vs0 = there >= 4 ? vs0 : there <= 0 ? 0 : vs0 & ((1u << (8 * there)) - 1);
-    vs1 = there >= 8 ? vs1 : there <= 4 ? 0 : vs1 & ((1u << (8 * (there - 4))) - 1);
   }
   float top[RB];
   bool up = false;
@@ -495,7 +605,6 @@ __device__ __forceinline__ void attend(const AttnArgs& a, Wave<D, RB, T>& w, con
       for (int f = 0; f < NF; ++f) w.o[f][rb] *= shrink;
     }
   }
-  u32 p[TERMS][RB][4];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
@@ -506,42 +615,18 @@ __device__ __forceinline__ void attend(const AttnArgs& a, Wave<D, RB, T>& w, con
       u32 t[TERMS];
       split_pair<TERMS>(e0, e1, t);
 #pragma unroll
-      for (int k = 0; k < TERMS; ++k) p[k][rb][h] = t[k];
+      for (int k = 0; k < TERMS; ++k) y.p[k][rb][h] = t[k];
     }
   }
   __builtin_amdgcn_sched_barrier(0);
-  u32 vs[8];
-  vs[0] = scale_at<0>(vs0); vs[1] = scale_at<1>(vs0); vs[2] = scale_at<2>(vs0); vs[3] = scale_at<3>(vs0);
-  vs[4] = scale_at<0>(vs1); vs[5] = scale_at<1>(vs1); vs[6] = scale_at<2>(vs1); vs[7] = scale_at<3>(vs1);
-  auto product = [&](int f, u32 v0, u32 v1, u32 v2, u32 v3) {
-    const bf16x8 v = as_bf16x8(v0, v1, v2, v3);
+}
+template <int D, int RB, typename T>
+__device__ __forceinline__ void add_values(Wave<D, RB, T>& w, const Weights<D, RB, T>& y, int n, bf16x8 values) {
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb)
+  for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-      for (int t = TERMS - 1; t >= 0; --t)
-        w.o[f][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, as_bf16x8(p[t][rb][0], p[t][rb][1], p[t][rb][2], p[t][rb][3]), w.o[f][rb], 0, 0, 0);
-  };
-  auto pairs = [&](auto byte, int f, const u32* words, u32 shift) {  // channels 2 byte, 2 byte + 1 of a dword column
-    constexpr int BYTE = decltype(byte)::value;
-    u32 y[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = decode<BYTE>(words[j] >> shift, vs[j]);
-    product(f, low_halves(y[0], y[1]), low_halves(y[2], y[3]), low_halves(y[4], y[5]), low_halves(y[6], y[7]));
-    product(f + 1, high_halves(y[0], y[1]), high_halves(y[2], y[3]), high_halves(y[4], y[5]), high_halves(y[6], y[7]));
-  };
-  if constexpr (D == 64) {
-    const u32 shift = (r & 1) * 16;
-    pairs(std::integral_constant<int, 0>{}, 0, x.v, shift);
-    pairs(std::integral_constant<int, 1>{}, 2, x.v, shift);
-  } else {
-#pragma unroll
-    for (int h = 0; h < D / 128; ++h) {
-      pairs(std::integral_constant<int, 0>{}, 8 * h, x.v + 8 * h, 0);
-      pairs(std::integral_constant<int, 1>{}, 8 * h + 2, x.v + 8 * h, 0);
-      pairs(std::integral_constant<int, 2>{}, 8 * h + 4, x.v + 8 * h, 0);
-      pairs(std::integral_constant<int, 3>{}, 8 * h + 6, x.v + 8 * h, 0);
-    }
-  }
+    for (int t = Wave<D, RB, T>::TERMS - 1; t >= 0; --t)
+      w.o[n][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values, as_bf16x8(y.p[t][rb][0], y.p[t][rb][1], y.p[t][rb][2], y.p[t][rb][3]), w.o[n][rb], 0, 0, 0);
 }
 
 // Where the results of a lane go: element [f][i] of its row among the 16 from `row0` on is channel (4g + i) * D/16 + f0 + f.
@@ -610,19 +695,21 @@ template <int MODE, int RB> constexpr int rows_per_block = MODE == KEYS ? 16 * R
 // Work-groups that have to fit a compute unit beside each other: what the compiler may give a wave of registers, and the ring of LDS.
 constexpr int per_unit(int D, int RB, bool f32) { return D == 256 ? (RB == 1 && !f32 ? 2 : 1) : f32 ? 2 : RB == 1 ? 3 : 2; }
 template <int D, int RB, typename T> constexpr int kPerUnit = per_unit(D, RB, std::is_same<T, float>::value);
-constexpr int stages_of(int D, int groups) {  // units in the ring, the one that is worked on among them
-  const int n = (160 * 1024 / groups - 1024) / (kWaves * (32 * D + (D <= 128 ? 256 : 512)));
+constexpr int values_bytes(int D, int mode) { return mode == ROWS ? kWaves * (D / 16) * 1024 : 0; }  // of a unit's values as operands
+constexpr int stages_of(int D, int mode, int groups) {  // units in the ring, the one that is worked on among them
+  const int n = (160 * 1024 / groups - 1024 - values_bytes(D, mode)) / (kWaves * (32 * D + (D <= 128 ? 256 : 512)));
   return n > 4 ? 4 : n;
 }
 
 template <int D, int RB, typename T, int MODE, bool UNIFORM>
 __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kernel(AttnArgs a) {
   using X = Tile<D>;
-  constexpr int NF = D / 16, STAGES = stages_of(D, kPerUnit<D, RB, T>);
+  constexpr int NF = D / 16, STAGES = stages_of(D, MODE, kPerUnit<D, RB, T>);
   static_assert(STAGES >= 2, "a unit in flight while another is worked on");
   constexpr int kJoin = MODE == KEYS ? 2 * RB * NF * 1024 : 0;  // bytes for two waves' results
   constexpr int kRing = STAGES * kWaves * X::kBytes;
   __shared__ __attribute__((aligned(1024))) uint8_t sh_ring[kRing > kJoin ? kRing : kJoin];
+  __shared__ __attribute__((aligned(16))) u32x4 sh_values[MODE == ROWS ? kWaves : 1][MODE == ROWS ? NF : 1][kWave];
   __shared__ u32 sh_bad[STAGES][kWaves];
   __shared__ float sh_m[MODE == KEYS ? 4 : 1][16 * RB], sh_l[MODE == KEYS ? 4 : 1][16 * RB];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
@@ -676,13 +763,45 @@ __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kern
       if (MODE == ROWS) __builtin_amdgcn_s_barrier();
       if (unit + STAGES - 1 < units) issue(stage == 0 ? STAGES - 1 : stage - 1);
       const int t_unit = from + unit * kUnit;
-#pragma unroll 1
-      for (int i = MODE == KEYS ? wave : 0; i < (MODE == KEYS ? wave + 1 : kWaves); ++i) {
-        const int t0 = t_unit + i * kTile;
-        if (t0 >= limit) break;
-        const u32 bad = __builtin_amdgcn_readfirstlane(sh_bad[stage][i]);
-        const Share<D> x(sh_ring + (stage * kWaves + i) * X::kBytes);
-        attend<D, RB, T>(a, w, x, t0 + kTile <= len && bad == 0, p.b, len, n, t0, bad >> g & 1);
+      if constexpr (MODE == KEYS) {
+        const int t0 = t_unit + wave * kTile;
+        if (t0 < limit) {
+          const uint8_t* tile = sh_ring + (stage * kWaves + wave) * X::kBytes;
+          const u32 bad = __builtin_amdgcn_readfirstlane(sh_bad[stage][wave]);
+          const bool plain = t0 + kTile <= len && bad == 0, poison = bad >> g & 1;
+          const Keys<D> keys(tile);
+          Values<D> values(tile);
+          Weights<D, RB, T> y;
+          weigh<D, RB, T>(a, w, keys, plain, p.b, len, n, t0, poison, y);
+          if (!plain) values.cut(poison ? 0 : end - t0 - 8 * g);
+          values.each([&](int f, bf16x8 v) { add_values<D, RB, T>(w, y, f, v); });
+        }
+      } else {
+        // Each wave converts the values of its tile for all.
+        {
+          const int t0 = t_unit + wave * kTile;
+          const u32 bad = __builtin_amdgcn_readfirstlane(sh_bad[stage][wave]);
+          Values<D> values(sh_ring + (stage * kWaves + wave) * X::kBytes);
+          if (t0 + kTile > end || bad) values.cut(bad >> g & 1 ? 0 : end - t0 - 8 * g);
+          values.each([&](int f, bf16x8 v) { sh_values[wave][f][lane] = __builtin_bit_cast(u32x4, v); });
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (what is in flight from memory stays so)
+        // (the values' operands are read in front of the scores, the next tile's keys in front of the product with the values)
+        Keys<D> keys(sh_ring + stage * kWaves * X::kBytes);
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+          const int t0 = t_unit + i * kTile;
+          if (t0 >= limit) break;
+          const u32 bad = __builtin_amdgcn_readfirstlane(sh_bad[stage][i]);
+          u32x4 v[NF];
+#pragma unroll
+          for (int f = 0; f < NF; ++f) v[f] = sh_values[i][f][lane];
+          Weights<D, RB, T> y;
+          weigh<D, RB, T>(a, w, keys, t0 + kTile <= len && bad == 0, p.b, len, n, t0, bad >> g & 1, y);
+          if (i + 1 < kWaves) keys = Keys<D>(sh_ring + (stage * kWaves + i + 1) * X::kBytes);
+#pragma unroll
+          for (int f = 0; f < NF; ++f) add_values<D, RB, T>(w, y, f, __builtin_bit_cast(bf16x8, v[f]));
+        }
       }
       stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
