@@ -91,13 +91,14 @@ static AttnPlan attn_plan(int N, int group, int dim, int dtype) {
 }
 // Blocks of so few units (as far as the caller says) are not cut: their pieces would have to be joined by a second kernel.
 constexpr int kWholeUnits = 8;
+constexpr int kMergeRows = 4;
 
 template <int D, int RB, typename T, int MODE> static int launch_attention(u32 groups, const AttnArgs& a, hipStream_t stream) {
   if (a.c.log_page >= 5) hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE, true>), dim3(groups), dim3(kThreads), 0, stream, a);
   else hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE, false>), dim3(groups), dim3(kThreads), 0, stream, a);
   if (hipGetLastError() != hipSuccess) return MARS_ERR_HIP;
   if (a.whole) return MARS_OK;
-  hipLaunchKernelGGL((merge_kernel<D, RB, T, MODE>), dim3(groups - 1, MODE == ROWS ? 4 * RB : RB), dim3(kThreads), 0, stream, a, groups);
+  hipLaunchKernelGGL((merge_kernel<D, RB, T, MODE>), dim3(groups - 1, MODE == ROWS ? kMergeRows : RB), dim3(kThreads), 0, stream, a, groups);
   return launched();
 }
 
@@ -209,7 +210,6 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
   a.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
   a.B = B; a.N = N; a.q_heads = q_heads; a.group = q_heads / c.heads; a.words = (N + 63) / 64;
   a.nodes = p.nodes;
-  a.least = 1;
   const long most_len = static_cast<long>(c.width) << c.log_page, blocks = static_cast<long>(B) * c.heads * ((N + p.nodes - 1) / p.nodes);
   const double units = static_cast<double>(blocks) * ((most_len + N + 3 * kUnit) / kUnit);  // at most; counted in 32 bits
   if (units > 4.0e9) return MARS_ERR_ARG;

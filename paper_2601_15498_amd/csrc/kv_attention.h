@@ -50,8 +50,7 @@ struct AttnArgs {
   float scale_log2;
   int B, N, q_heads, group, words;
   int nodes;    // of a block of rows
-  bool whole;   // the deal gives out whole blocks
-  u32 least;    // units a work-group takes at least
+  bool whole;   // the deal gives out whole items
 };
 
 __device__ __forceinline__ float max3(float a, float b, float c) {  // (written out: fmaxf would first quiet each operand)
@@ -87,7 +86,7 @@ template <int TERMS> __device__ __forceinline__ void split_pair(float a, float b
 // ---------------------------------------------------------------- the deal
 // A request's items are (cache head, block of `nodes` nodes), its units those of its items.  Under a mask a block has all the request's keys.
 // In a chain it has those up to its last node, and blocks are taken in pairs, the last with the first and so on, so that every pair has about
-// the same number of units: `per`, which is rounded up (what is left over of it is idle).  Where whole blocks are given out, one counts as a unit.
+// the same number of units: `per`, which is rounded up (what is left over of it is idle).
 struct Request {
   int n, len, blocks, pairs;  // pairs: of blocks, or blocks
   u32 per;                    // units of a pair, or of a block
@@ -99,16 +98,15 @@ struct Request {
     if (s >= 0) len = min(max(a.c.lens[s], 0), a.c.width << a.c.log_page);
     else n = 0;
     blocks = (n + a.nodes - 1) / a.nodes;
-    const bool paired = !a.mask && !a.whole && blocks > 1;
+    const bool paired = !a.mask && blocks > 1;
     pairs = paired ? (blocks + 1) / 2 : blocks;
-    per = a.whole ? 1 : paired ? (2u * len + static_cast<u32>(blocks + 1) * a.nodes + 2 * (kUnit - 1)) / kUnit : static_cast<u32>(len + n + kUnit - 1) / kUnit;
+    per = paired ? (2u * len + static_cast<u32>(blocks + 1) * a.nodes + 2 * (kUnit - 1)) / kUnit : static_cast<u32>(len + n + kUnit - 1) / kUnit;
   }
-  __device__ __forceinline__ u32 units(const AttnArgs& a) const { return static_cast<u32>(a.c.heads) * pairs * per; }
+  __device__ __forceinline__ u32 items(const AttnArgs& a) const { return static_cast<u32>(a.c.heads) * pairs; }
   // Keys that a block's rows see at most.
   __device__ __forceinline__ int keys(const AttnArgs& a, int block) const { return len + (a.mask ? n : min(n, (block + 1) * a.nodes)); }
   __device__ __forceinline__ u32 block_units(const AttnArgs& a, int block) const { return static_cast<u32>(keys(a, block) + kUnit - 1) / kUnit; }
 };
-// Units before the one a place in the deal begins with, sums over a wave's lanes.
 __device__ __forceinline__ u32 wave_scan(u32 v) {
   const int lane = threadIdx.x % kWave;
 #pragma unroll
@@ -118,32 +116,55 @@ __device__ __forceinline__ u32 wave_scan(u32 v) {
   }
   return v;
 }
-// A place in the deal, kept by every wave for itself: 64 requests at a time, one per lane.
+__device__ __forceinline__ u32 wave_max(u32 v) {
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) v = max(v, static_cast<u32>(__shfl_xor(static_cast<int>(v), d)));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+// What a work-group's share of the units comes to, and a place in the deal, kept by every wave for itself: 64 requests at a time, one per lane.
+// Where no work-group gets much more by it (kJoinCost), whole items are given out and none is cut: then an item counts as two, one for each
+// of its blocks.
+constexpr u32 kJoinCost = 8;  // units; two prompts of 2 048, every pair of blocks with a work-group of its own: 50 units instead of 45, and the
+                              // pieces' 134 MB neither written nor read
 struct Deal {
   const AttnArgs& a;
   Request mine;       // of request first + lane
   int first;
   u32 front, before;  // units in front of the 64, in front of the lane's request
   u32 sum;            // of the 64
-  u32 total;
-  __device__ __forceinline__ void load(int b0, u32 units_in_front) {
-    first = b0;
+  u32 total, share;
+  bool whole;
+  __device__ __forceinline__ u32 units(const Request& r) const { return whole ? 2 * r.items(a) : r.items(a) * r.per; }
+  __device__ __forceinline__ void place(u32 units_in_front) {
     front = units_in_front;
-    const int b = b0 + threadIdx.x % kWave;
-    mine = Request(a, min(b, a.B - 1));
-    const u32 units = b < a.B ? mine.units(a) : 0;
-    const u32 x = wave_scan(units);
-    before = front + x - units;
+    const u32 v = first + static_cast<int>(threadIdx.x % kWave) < a.B ? units(mine) : 0;
+    const u32 x = wave_scan(v);
+    before = front + x - v;
     sum = __builtin_amdgcn_readlane(x, kWave - 1);
   }
-  __device__ __forceinline__ explicit Deal(const AttnArgs& args) : a(args) {
-    load(0, 0);
-    total = sum;
-    for (int b = kWave; b < a.B; b += kWave) {
-      const int b1 = b + threadIdx.x % kWave;
-      const u32 units = b1 < a.B ? Request(a, b1).units(a) : 0;
-      total += __builtin_amdgcn_readlane(wave_scan(units), kWave - 1);
+  __device__ __forceinline__ void load(int b0) {
+    first = b0;
+    mine = Request(a, min(b0 + static_cast<int>(threadIdx.x % kWave), a.B - 1));
+  }
+  __device__ __forceinline__ Deal(const AttnArgs& args, u32 groups) : a(args) {
+    u32 items = 0, most = 0;
+    total = 0;
+    whole = false;
+    for (int b = a.B - 1 & ~(kWave - 1); b >= 0; b -= kWave) {  // (ends at the first 64)
+      load(b);
+      const bool in = b + static_cast<int>(threadIdx.x % kWave) < a.B;
+      items += __builtin_amdgcn_readlane(wave_scan(in ? mine.items(a) : 0), kWave - 1);
+      total += __builtin_amdgcn_readlane(wave_scan(in ? mine.items(a) * mine.per : 0), kWave - 1);
+      most = max(most, wave_max(in && mine.items(a) ? mine.per : 0));
     }
+    share = (total + groups - 1) / groups;
+    const u32 each = (items + groups - 1) / groups;
+    whole = a.whole || each * most <= share + kJoinCost;
+    if (whole) {
+      share = 2 * each;
+      total = 2 * items;
+    }
+    place(0);
   }
   // The block that unit u (not before an earlier call's) belongs to.
   struct Place {
@@ -153,7 +174,10 @@ struct Deal {
     Request r;
   };
   __device__ __forceinline__ Place find(u32 u) {
-    while (u >= front + sum) load(first + kWave, front + sum);  // (u < total: there are more)
+    while (u >= front + sum) {  // (u < total: there are more)
+      load(first + kWave);
+      place(front + sum);
+    }
     const unsigned long long at = __ballot(before <= u && first + static_cast<int>(threadIdx.x % kWave) < a.B);
     // the last that begins at u or before; those without units that begin there too come before it or not at all
     const int lane = 63 - __builtin_clzll(at);
@@ -164,33 +188,29 @@ struct Deal {
     p.r.blocks = __builtin_amdgcn_readlane(mine.blocks, lane);
     p.r.pairs = __builtin_amdgcn_readlane(mine.pairs, lane);
     p.r.per = __builtin_amdgcn_readlane(mine.per, lane);
-    const u32 local = u - __builtin_amdgcn_readlane(before, lane);
-    const u32 item = local / p.r.per, in = local % p.r.per;
+    const u32 local = u - __builtin_amdgcn_readlane(before, lane), per = whole ? 2 : p.r.per;
+    const u32 item = local / per, in = local % per;
     p.head = item / p.r.pairs;
     p.block = item % p.r.pairs;
+    const bool paired = p.r.pairs != p.r.blocks;  // (one block alone is no pair)
+    const int late = paired ? p.r.blocks - 1 - p.block : p.block;
+    const u32 those = whole ? 1 : paired ? p.r.block_units(a, late) : per;
     p.offset = in;
-    if (p.r.pairs == p.r.blocks) {  // (one block alone is no pair)
-      p.count = p.r.per;
+    if (in < those) {
+      p.block = late;
+      p.count = those;
     } else {
-      const int late = p.r.blocks - 1 - p.block;
-      const u32 those = p.r.block_units(a, late);
-      if (in < those) {
-        p.block = late;
-        p.count = those;
-      } else {
-        p.offset = in - those;
-        p.count = late == p.block ? 0 : p.r.block_units(a, p.block);
-        if (p.offset >= p.count) {
-          p.count = 0;
-          p.offset = p.r.per - in;
-        }
+      p.offset = in - those;
+      p.count = late == p.block ? 0 : whole ? 1 : p.r.block_units(a, p.block);
+      if (p.offset >= p.count) {
+        p.count = 0;
+        p.offset = per - in;
       }
     }
     p.begin = u - p.offset;
     return p;
   }
 };
-__device__ __forceinline__ u32 share_of(u32 total, u32 groups, u32 least) { return max((total + groups - 1) / groups, least); }
 
 // ---------------------------------------------------------------- tiles on their way through LDS
 // A tile of 32 keys in LDS: codes of the keys, codes of the values, then the scales of both.  Sixteen bytes go from memory to LDS per lane and
@@ -562,12 +582,10 @@ template <int D, int RB, typename T> struct Weights { u32 p[Wave<D, RB, T>::TERM
 // One tile.  `plain` (the same for the wave): every row sees all of it, and all of it is there.  Otherwise: request b has n nodes behind
 // `len` tokens, the tile begins at t0; `poison`: the lane's octet has no page.
 template <int D, int RB, typename T>
-__device__ __forceinline__ void weigh(const AttnArgs& a, Wave<D, RB, T>& w, const Keys<D>& x, bool plain, int b, int len, int n, int t0, bool poison,
+__device__ __forceinline__ void weigh(const AttnArgs& a, Wave<D, RB, T>& w, f32x4 (&sc)[2][RB], bool plain, int b, int len, int n, int t0, bool poison,
                                       Weights<D, RB, T>& y) {
   constexpr int NF = D / 16, TERMS = Wave<D, RB, T>::TERMS;
   const float c = a.scale_log2;
-  f32x4 sc[2][RB];
-  w.q.scores(x, sc);
   __builtin_amdgcn_sched_barrier(0);  // (the values' conversions would be brought up to here, and their results kept)
   if (!plain) {
     const int first = t0 + static_cast<int>(threadIdx.x % kWave / 16) * 8 - len;
@@ -719,8 +737,8 @@ __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kern
       const int n = Request(a, b).n;
       if (n < a.N) clear_rows<T, D>(a, b, n);
     }
-  Deal deal(a);
-  const u32 share = share_of(deal.total, gridDim.x, a.least);
+  Deal deal(a, gridDim.x);
+  const u32 share = deal.share;
   // neighbours in the deal on the same die (block index mod 8)
   const u32 per_die = gridDim.x >> 3;
   const u32 group = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3);
@@ -738,7 +756,7 @@ __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kern
     }
     const u32 taken = min(p.count - p.offset, unit1 - u);
     const bool whole = taken == p.count;
-    const int units = static_cast<int>(a.whole ? p.r.block_units(a, p.block) : taken);
+    const int units = static_cast<int>(deal.whole ? p.r.block_units(a, p.block) : taken);
     const int node0 = p.block * a.nodes, rows = min(a.nodes, p.r.n - node0) * a.group, row0 = MODE == ROWS ? wave * 16 * RB : 0;
     const int len = p.r.len, n = p.r.n, end = len + n;
     // no row of this wave sees keys from here on (-1: it has no rows)
@@ -771,8 +789,10 @@ __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kern
           const bool plain = t0 + kTile <= len && bad == 0, poison = bad >> g & 1;
           const Keys<D> keys(tile);
           Values<D> values(tile);
+          f32x4 sc[2][RB];
+          w.q.scores(keys, sc);
           Weights<D, RB, T> y;
-          weigh<D, RB, T>(a, w, keys, plain, p.b, len, n, t0, poison, y);
+          weigh<D, RB, T>(a, w, sc, plain, p.b, len, n, t0, poison, y);
           if (!plain) values.cut(poison ? 0 : end - t0 - 8 * g);
           values.each([&](int f, bf16x8 v) { add_values<D, RB, T>(w, y, f, v); });
         }
@@ -786,8 +806,10 @@ __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kern
           values.each([&](int f, bf16x8 v) { sh_values[wave][f][lane] = __builtin_bit_cast(u32x4, v); });
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (what is in flight from memory stays so)
-        // (the values' operands are read in front of the scores, the next tile's keys in front of the product with the values)
-        Keys<D> keys(sh_ring + stage * kWaves * X::kBytes);
+        // A tile's scores are under way on the matrix cores while the one before it is weighed.
+        const uint8_t* const tiles = sh_ring + stage * kWaves * X::kBytes;
+        f32x4 sc[2][2][RB];
+        w.q.scores(Keys<D>(tiles), sc[0]);
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) {
           const int t0 = t_unit + i * kTile;
@@ -796,9 +818,9 @@ __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kern
           u32x4 v[NF];
 #pragma unroll
           for (int f = 0; f < NF; ++f) v[f] = sh_values[i][f][lane];
+          if (i + 1 < kWaves) w.q.scores(Keys<D>(tiles + (i + 1) * X::kBytes), sc[(i + 1) % 2]);
           Weights<D, RB, T> y;
-          weigh<D, RB, T>(a, w, keys, t0 + kTile <= len && bad == 0, p.b, len, n, t0, bad >> g & 1, y);
-          if (i + 1 < kWaves) keys = Keys<D>(sh_ring + (stage * kWaves + i + 1) * X::kBytes);
+          weigh<D, RB, T>(a, w, sc[i % 2], t0 + kTile <= len && bad == 0, p.b, len, n, t0, bad >> g & 1, y);
 #pragma unroll
           for (int f = 0; f < NF; ++f) add_values<D, RB, T>(w, y, f, __builtin_bit_cast(bf16x8, v[f]));
         }
@@ -884,8 +906,9 @@ __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kern
 template <int D, int RB, typename T, int MODE>
 __global__ void __launch_bounds__(kThreads) merge_kernel(AttnArgs a, u32 groups) {
   constexpr int NF = D / 16, F = NF / 4, AT_ONCE = D == 256 ? 4 : 8;
-  Deal deal(a);
-  const u32 share = share_of(deal.total, groups, a.least);
+  Deal deal(a, groups);
+  if (deal.whole) return;
+  const u32 share = deal.share;
   const u32 cut = blockIdx.x + 1;
   const unsigned long long at = static_cast<unsigned long long>(cut) * share;
   if (at >= deal.total) return;
@@ -895,9 +918,11 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(AttnArgs a, u32 groups)
   if (cut != first + 1) return;                       // an earlier cut's
   const int node0 = p.block * a.nodes, rows = min(a.nodes, p.r.n - node0) * a.group;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 16;
-  const int strip = blockIdx.y, f0 = wave * F;         // of 16 rows
+  const int f0 = wave * F;
+  constexpr int STRIPS = MODE == ROWS ? 4 * RB : RB;  // of 16 rows
+  for (int strip = blockIdx.y; strip < STRIPS; strip += gridDim.y) {
   const int part = MODE == ROWS ? strip / RB : 0, rb = MODE == ROWS ? strip % RB : strip;
-  if (part * 16 * RB + rb * 16 >= rows) return;
+  if (strip * 16 >= rows) break;
   float m = kFloor, l = 0.0f;
   f32x4 o[F];
 #pragma unroll
@@ -932,7 +957,8 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(AttnArgs a, u32 groups)
       }
     }
   }
-  write_part<D, F, T>(a, p.b, p.head, node0, part * 16 * RB + rb * 16, rows, f0, o, m, l);
+  write_part<D, F, T>(a, p.b, p.head, node0, strip * 16, rows, f0, o, m, l);
+  }
 }
 
 }  // namespace kv
