@@ -107,19 +107,25 @@ struct Request {
   __device__ __forceinline__ int keys(const AttnArgs& a, int block) const { return len + (a.mask ? n : min(n, (block + 1) * a.nodes)); }
   __device__ __forceinline__ u32 block_units(const AttnArgs& a, int block) const { return static_cast<u32>(keys(a, block) + kUnit - 1) / kUnit; }
 };
+// Over the wave's lanes, lane 0 first: inside each row of 16 by shifts, then the rows in front through scalar registers (a scan by exchanges
+// through LDS took a microsecond of every launch).  A lane whose source falls outside its row gets 0.
 __device__ __forceinline__ u32 wave_scan(u32 v) {
-  const int lane = threadIdx.x % kWave;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const u32 y = __shfl_up(v, d);
-    if (lane >= d) v += y;
-  }
-  return v;
+  v += dpp<0x111>(v);  // row_shr 1, 2, 4, 8
+  v += dpp<0x112>(v);
+  v += dpp<0x114>(v);
+  v += dpp<0x118>(v);
+  const u32 t0 = __builtin_amdgcn_readlane(v, 15), t1 = __builtin_amdgcn_readlane(v, 31), t2 = __builtin_amdgcn_readlane(v, 47);
+  const u32 row = threadIdx.x % kWave / 16;
+  return v + (row > 0 ? t0 : 0) + (row > 1 ? t1 : 0) + (row > 2 ? t2 : 0);
 }
+__device__ __forceinline__ u32 wave_sum(u32 v) { return __builtin_amdgcn_readlane(wave_scan(v), kWave - 1); }
 __device__ __forceinline__ u32 wave_max(u32 v) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) v = max(v, static_cast<u32>(__shfl_xor(static_cast<int>(v), d)));
-  return __builtin_amdgcn_readfirstlane(v);
+  v = max(v, dpp<0x111>(v));
+  v = max(v, dpp<0x112>(v));
+  v = max(v, dpp<0x114>(v));
+  v = max(v, dpp<0x118>(v));
+  return max(max(static_cast<u32>(__builtin_amdgcn_readlane(v, 15)), static_cast<u32>(__builtin_amdgcn_readlane(v, 31))),
+             max(static_cast<u32>(__builtin_amdgcn_readlane(v, 47)), static_cast<u32>(__builtin_amdgcn_readlane(v, 63))));
 }
 // What a work-group's share of the units comes to, and a place in the deal, kept by every wave for itself: 64 requests at a time, one per lane.
 // Where no work-group gets much more by it (kJoinCost), whole items are given out and none is cut: then an item counts as two, one for each
@@ -153,8 +159,8 @@ struct Deal {
     for (int b = a.B - 1 & ~(kWave - 1); b >= 0; b -= kWave) {  // (ends at the first 64)
       load(b);
       const bool in = b + static_cast<int>(threadIdx.x % kWave) < a.B;
-      items += __builtin_amdgcn_readlane(wave_scan(in ? mine.items(a) : 0), kWave - 1);
-      total += __builtin_amdgcn_readlane(wave_scan(in ? mine.items(a) * mine.per : 0), kWave - 1);
+      items += wave_sum(in ? mine.items(a) : 0);
+      total += wave_sum(in ? mine.items(a) * mine.per : 0);
       most = max(most, wave_max(in && mine.items(a) ? mine.per : 0));
     }
     share = (total + groups - 1) / groups;
@@ -540,6 +546,7 @@ template <int D, int RB, typename T> struct Wave {
   f32x4 o[NF][RB];
   float m[RB], l[RB];
   int node[RB];                                 // of this lane's rows; < 0: no row
+  unsigned long long word[RB];                  // the row's mask, where it is one word
 
   // Rows row0 .. of the block of nodes from node0 on, which has `rows`.
   __device__ __forceinline__ void start(const AttnArgs& a, int b, int head, int node0, int row0, int rows) {
@@ -550,6 +557,7 @@ template <int D, int RB, typename T> struct Wave {
       const bool live = row < rows;
       const int in = live ? row / a.group : 0, h = live ? row - in * a.group : 0;
       node[rb] = live ? node0 + in : -1;
+      word[rb] = a.mask && a.words == 1 ? a.mask[static_cast<size_t>(b) * a.N + node0 + in] : 0;
       q.load(rb, static_cast<const T*>(a.q) + b * a.q_request + static_cast<long>(node0 + in) * a.q_node + static_cast<long>(head * a.group + h) * a.q_head, live);
       m[rb] = kFloor;
       l[rb] = 0.0f;
@@ -559,12 +567,13 @@ template <int D, int RB, typename T> struct Wave {
   }
 };
 
-// Which of the keys first .. first + 7 (numbered from the first node on; committed ones are < 0) row `node` of n nodes sees.
-__device__ __forceinline__ u32 seen(const AttnArgs& a, int b, int node, int n, int first) {
+// Which of the keys first .. first + 7 (numbered from the first node on; committed ones are < 0) row `node` of n nodes sees.  `only`: its mask, if that
+// is one word.
+__device__ __forceinline__ u32 seen(const AttnArgs& a, unsigned long long only, int b, int node, int n, int first) {
   u32 bits;
   if (a.mask) {
     const unsigned long long* row = a.mask + (static_cast<size_t>(b) * a.N + node) * a.words;
-    auto word = [&](int w) { return w < 0 ? ~0ull : w < a.words ? row[w] : 0ull; };
+    auto word = [&](int w) { return w < 0 ? ~0ull : w >= a.words ? 0ull : a.words == 1 ? only : row[w]; };
     const int w = first >> 6, shift = first & 63;
     bits = static_cast<u32>(word(w) >> shift);
     if (shift > 56) bits |= static_cast<u32>(word(w + 1) << (64 - shift));
@@ -591,7 +600,7 @@ __device__ __forceinline__ void weigh(const AttnArgs& a, Wave<D, RB, T>& w, f32x
     const int first = t0 + static_cast<int>(threadIdx.x % kWave / 16) * 8 - len;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      const u32 sees = w.node[rb] < 0 ? 0u : seen(a, b, w.node[rb], n, first);
+      const u32 sees = w.node[rb] < 0 ? 0u : seen(a, w.word[rb], b, w.node[rb], n, first);
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
