@@ -1,5 +1,5 @@
-"""Compile the HIP library (csrc/mars.hip, csrc/cache.hip) for gfx950 into paper_2601_15498_amd/libmars.so, and the native part
-of its Python binding (csrc/marshal.cpp) into paper_2601_15498_amd/_marshal.so."""
+"""Compile the HIP library (csrc/mars.hip, csrc/cache.hip) for gfx950 into paper_2601_15498_amd/libmars.so, and the native parts
+of its Python binding (csrc/marshal.cpp, csrc/cache_marshal.cpp) into _marshal.so and _cache_marshal.so beside it."""
 import os
 import subprocess
 import sys
@@ -12,6 +12,8 @@ OBJECTS = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmars.so")
 MARSHAL_SRC = os.path.join(HERE, "csrc", "marshal.cpp")
 MARSHAL_LIB = os.path.join(HERE, "_marshal.so")
+CACHE_MARSHAL_SRC = os.path.join(HERE, "csrc", "cache_marshal.cpp")
+CACHE_MARSHAL_LIB = os.path.join(HERE, "_cache_marshal.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -25,14 +27,14 @@ FLAGS = [
 SRC_FLAGS = ["-Xarch_device", "-fno-honor-nans"]
 
 
-def build_marshal(verbose: bool = False, out: str = MARSHAL_LIB, extra=()) -> str:
+def build_marshal(verbose: bool = False, out: str = MARSHAL_LIB, extra=(), src: str = MARSHAL_SRC) -> str:
     import sysconfig
     import torch
     from torch.utils.cpp_extension import include_paths
     include = [sysconfig.get_paths()["include"]] + [p for p in include_paths() if os.path.isdir(p)]
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DMARS_TORCH_VERSION="{torch.__version__}"']
-    cmd += ["-isystem" + p for p in include] + list(extra) + ["-o", out, MARSHAL_SRC]
+    cmd += ["-isystem" + p for p in include] + list(extra) + ["-o", out, src]
     cmd += ["-L" + os.path.join(os.path.dirname(torch.__file__), "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
     if verbose:
         print(" ".join(cmd), flush=True)
@@ -58,13 +60,14 @@ def build(verbose: bool = False, extra=()) -> str:
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
-    # The binding does without its native part where this machine cannot build it (no g++, no Python.h).
-    if os.path.exists(MARSHAL_LIB):
-        os.remove(MARSHAL_LIB)
-    try:
-        build_marshal(verbose)
-    except (OSError, subprocess.CalledProcessError) as e:
-        warnings.warn(f"{MARSHAL_LIB} was not built ({e}): calls will go through ctypes", RuntimeWarning)
+    # The binding does without its native parts where this machine cannot build them (no g++, no Python.h).
+    for out, src in ((MARSHAL_LIB, MARSHAL_SRC), (CACHE_MARSHAL_LIB, CACHE_MARSHAL_SRC)):
+        if os.path.exists(out):
+            os.remove(out)
+        try:
+            build_marshal(verbose, out, src=src)
+        except (OSError, subprocess.CalledProcessError) as e:
+            warnings.warn(f"{out} was not built ({e}): calls will go through ctypes", RuntimeWarning)
     return LIB
 
 

@@ -4,9 +4,13 @@ The functions mirror the header name for name and take the cache's tensors: ``po
 [sequences, width], ``lens``, ``held`` [sequences] and ``refs`` [pages], all int32 (``KVCache`` makes them).  Every call enqueues on the
 current torch stream and returns without synchronising; there is no CPU fallback.  bf16 rows may be given as ``torch.bfloat16`` or as
 ``torch.uint16``/``int16`` bit patterns.
+
+A regular call -- plain tensors of the right types and shapes, outputs and workspace given -- goes through csrc/cache_marshal.cpp
+(``_cache_marshal.so``); anything else through ctypes here, with the checks that say what is wrong.
 """
 import ctypes
 import math
+import warnings
 
 import torch
 
@@ -30,10 +34,36 @@ class RowsStruct(ctypes.Structure):
 
 
 _lib = None
+_native = None  # csrc/cache_marshal.cpp, once the library is loaded
+
+
+class _NoNative:
+    """In place of csrc/cache_marshal.cpp: no call is a regular one."""
+    append = read = tree_mask = attention = commit = reserve = fork = release = staticmethod(lambda *args: None)
+
+
+def _load_native(L):
+    try:
+        from . import _cache_marshal
+        if _cache_marshal.torch_version != torch.__version__:
+            raise ImportError(f"built with PyTorch {_cache_marshal.torch_version}, not {torch.__version__}")
+    except ImportError as e:
+        warnings.warn(f"_cache_marshal.so is missing or does not load ({e}): calls go through ctypes, which costs some 6 us each; "
+                      "build it with `python -m paper_2601_15498_amd.build`", RuntimeWarning, stacklevel=3)
+        return _NoNative
+    _cache_marshal.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in
+                          (L.mars_kv_append, L.mars_kv_read, L.mars_tree_mask, L.mars_kv_attention, L.mars_kv_commit, L.mars_kv_reserve,
+                           L.mars_kv_fork, L.mars_kv_release)), True)
+    return _cache_marshal
+
+
+def _calls():
+    lib()
+    return _native
 
 
 def lib():
-    global _lib
+    global _lib, _native
     if _lib is None:
         L = binding.lib()
         p, i, n = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
@@ -53,6 +83,7 @@ def lib():
                 ("mars_kv_copy_pages", i, [cache, p, p, i, p])):
             f = getattr(L, name)
             f.restype, f.argtypes = result, arguments
+        _native = _load_native(L)   # (before _lib: whoever sees the library has the calls)
         _lib = L
     return _lib
 
@@ -119,6 +150,9 @@ def mars_kv_append(pool: torch.Tensor, page_table: torch.Tensor, lens: torch.Ten
                    seqs: torch.Tensor = None, n_new: torch.Tensor = None, status: torch.Tensor = None) -> None:
     """Keys and values [B, N, heads, head_dim] of new tokens into the cache, behind the committed ones.  Any strides that are multiples of 16
     bytes, the last one 1."""
+    rc = (_native or _calls()).append(pool, page_table, lens, k, v, layer, seqs, n_new, status, _stream)
+    if rc is not None:
+        return _check(rc)
     B, N, heads, D = k.shape
     assert v.shape == k.shape and v.dtype == k.dtype and heads == pool.shape[2]
     c = _cache(pool, page_table, lens, head_dim=D, page_size=_page_size(pool, D))
@@ -130,6 +164,11 @@ def mars_kv_append(pool: torch.Tensor, page_table: torch.Tensor, lens: torch.Ten
 def mars_kv_read(pool: torch.Tensor, page_table: torch.Tensor, held: torch.Tensor = None, *, layer: int = 0, seqs: torch.Tensor = None,
                  first: torch.Tensor = None, out=None, B: int = None, N: int = None, head_dim: int = None, dtype=torch.bfloat16):
     """Keys and values [B, N, heads, head_dim] of positions first[b] .. first[b] + N - 1, into ``out`` (a pair) if given."""
+    if out is not None:
+        rc = (_native or _calls()).read(pool, page_table, held, *out, layer, seqs, first, _stream)
+        if rc is not None:
+            _check(rc)
+            return out
     if out is None:
         B = B if B is not None else seqs.numel() if seqs is not None else page_table.shape[0]
         out = tuple(torch.empty((B, N, pool.shape[2], head_dim), dtype=dtype, device=pool.device) for _ in range(2))
@@ -145,6 +184,10 @@ def mars_kv_read(pool: torch.Tensor, page_table: torch.Tensor, held: torch.Tenso
 def mars_tree_mask(tree_parent: torch.Tensor, *, n_new: torch.Tensor = None, mask: torch.Tensor = None,
                    status: torch.Tensor = None) -> torch.Tensor:
     """[B, N, (N + 63) // 64] int64: bit j of row i is set iff node j is node i or an ancestor."""
+    rc = (_native or _calls()).tree_mask(tree_parent, n_new, mask, status, _stream)
+    if rc is not None:
+        _check(rc)
+        return mask
     B, N = tree_parent.shape
     if mask is None:
         mask = torch.empty((B, N, (N + 63) // 64), dtype=torch.int64, device=tree_parent.device)
@@ -168,6 +211,10 @@ def mars_kv_attention(pool: torch.Tensor, page_table: torch.Tensor, lens: torch.
                       max_len: int = 0, out: torch.Tensor = None, lse: torch.Tensor = None, workspace: torch.Tensor = None):
     """Attention of queries [B, N, q_heads, head_dim] over the committed tokens and the nodes they see.  Returns (out, lse); lse is only
     formed where a tensor [B, N, q_heads] fp32 is given for it."""
+    rc = (_native or _calls()).attention(pool, page_table, lens, q, layer, seqs, n_new, mask, scale, max_len, out, lse, workspace, _stream)
+    if rc is not None:
+        _check(rc)
+        return out, lse
     B, N, q_heads, D = q.shape
     c = _cache(pool, page_table, lens, head_dim=D, page_size=_page_size(pool, D))
     if out is None:
@@ -189,9 +236,13 @@ def mars_kv_commit(pool: torch.Tensor, page_table: torch.Tensor, lens: torch.Ten
                    page_size: int, seqs: torch.Tensor = None, new_lens: torch.Tensor = None, status: torch.Tensor = None) -> torch.Tensor:
     """The accepted nodes' rows move up behind the committed tokens in every layer; returns the new lengths (``lens`` itself, updated, where no
     other tensor is given for them)."""
-    B, N = path_idx.shape
     if new_lens is None:
         new_lens = lens
+    rc = (_native or _calls()).commit(pool, page_table, lens, accept_len, path_idx, page_size, seqs, new_lens, status, _stream)
+    if rc is not None:
+        _check(rc)
+        return new_lens
+    B, N = path_idx.shape
     c = _cache(pool, page_table, lens, page_size=page_size)
     _check(lib().mars_kv_commit(c, _batch(seqs, lens, B), _table(accept_len, (B,), "accept_len"), _table(path_idx, (B, N), "path_idx"), B, N,
                                 _table(new_lens, lens.shape, "new_lens"), _table(status, (B,), "status"), _stream()))
@@ -209,6 +260,10 @@ def mars_kv_reserve(pool: torch.Tensor, page_table: torch.Tensor, lens: torch.Te
                     page_size: int, seqs: torch.Tensor = None, status: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
     """Room for n tokens (an int for all requests, or [B] int32) behind the committed ones; pages that others hold too are copied where they
     would be written.  Returns the status of every request."""
+    rc = (_native or _calls()).reserve(pool, page_table, lens, held, refs, n, page_size, seqs, status, workspace, _stream)
+    if rc is not None:
+        _check(rc)
+        return status
     n_new = n if isinstance(n, torch.Tensor) else None
     B = seqs.numel() if seqs is not None else n_new.numel() if n_new is not None else lens.numel()
     if status is None:
@@ -224,6 +279,9 @@ def mars_kv_reserve(pool: torch.Tensor, page_table: torch.Tensor, lens: torch.Te
 def mars_kv_fork(page_table: torch.Tensor, lens: torch.Tensor, held: torch.Tensor, refs: torch.Tensor, src: torch.Tensor, dst: torch.Tensor, *,
                  page_size: int, status: torch.Tensor = None) -> None:
     """Empty sequences dst[b] become copies of src[b] that share the pages of the committed tokens."""
+    rc = (_native or _calls()).fork(page_table, lens, held, refs, src, dst, page_size, status, _stream)
+    if rc is not None:
+        return _check(rc)
     B = src.numel()
     c = _cache(None, page_table, lens, held, refs, page_size=page_size)
     _check(lib().mars_kv_fork(c, _table(src, (B,), "src"), _table(dst, (B,), "dst"), B, _table(status, (B,), "status"), _stream()))
@@ -232,6 +290,9 @@ def mars_kv_fork(page_table: torch.Tensor, lens: torch.Tensor, held: torch.Tenso
 def mars_kv_release(page_table: torch.Tensor, lens: torch.Tensor, held: torch.Tensor, refs: torch.Tensor, seqs: torch.Tensor, *,
                     status: torch.Tensor = None) -> None:
     """The sequences give their pages back."""
+    rc = (_native or _calls()).release(page_table, lens, held, refs, seqs, status, _stream)
+    if rc is not None:
+        return _check(rc)
     B = seqs.numel()
     c = _cache(None, page_table, lens, held, refs, page_size=8)
     _check(lib().mars_kv_release(c, _table(seqs, (B,), "seqs"), B, _table(status, (B,), "status"), _stream()))
