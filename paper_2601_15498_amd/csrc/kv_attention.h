@@ -806,7 +806,11 @@ __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kern
           values.each([&](int f, bf16x8 v) { add_values<D, RB, T>(w, y, f, v); });
         }
       } else {
-        // Each wave converts the values of its tile for all.
+        // A tile's scores are under way on the matrix cores while the one before it is weighed, the first one's while each wave
+        // converts the values of its tile for all.
+        const uint8_t* const tiles = sh_ring + stage * kWaves * X::kBytes;
+        f32x4 sc[2][2][RB];
+        w.q.scores(Keys<D>(tiles), sc[0]);
         {
           const int t0 = t_unit + wave * kTile;
           const u32 bad = __builtin_amdgcn_readfirstlane(sh_bad[stage][wave]);
@@ -815,10 +819,6 @@ __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kern
           values.each([&](int f, bf16x8 v) { sh_values[wave][f][lane] = __builtin_bit_cast(u32x4, v); });
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (what is in flight from memory stays so)
-        // A tile's scores are under way on the matrix cores while the one before it is weighed.
-        const uint8_t* const tiles = sh_ring + stage * kWaves * X::kBytes;
-        f32x4 sc[2][2][RB];
-        w.q.scores(Keys<D>(tiles), sc[0]);
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) {
           const int t0 = t_unit + i * kTile;
