@@ -59,6 +59,7 @@ template <typename F> static int by_type(int dtype, F f) { return dtype == MARS_
 static int row_octets(int N) { return (N + 6) / 8 + 1; }  // octets that N positions can touch
 
 constexpr int kCommitGroups = 2048;
+constexpr int kPlanFewPages = 16384;  // four steps of the search
 
 // ---------------------------------------------------------------- attention: how the work is laid out
 struct AttnPlan {
@@ -260,7 +261,10 @@ int mars_kv_reserve(const mars_kv_cache* cache, const int32_t* seqs, const int32
     return MARS_ERR_WORKSPACE;
   const ReserveSpace ws = reserve_space(static_cast<char*>(workspace), B);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kPlanThreads), 0, stream, c, seqs, n_new, B, N, status, ws);
+  if (B <= kPlanFew && c.pages <= kPlanFewPages)
+    hipLaunchKernelGGL(reserve_kernel<kPlanFew>, dim3(1), dim3(kPlanFew), 0, stream, c, seqs, n_new, B, N, status, ws);
+  else
+    hipLaunchKernelGGL(reserve_kernel<kPlanMany>, dim3(1), dim3(kPlanMany), 0, stream, c, seqs, n_new, B, N, status, ws);
   if (hipGetLastError() != hipSuccess) return MARS_ERR_HIP;
   hipLaunchKernelGGL(copy_pages_kernel, dim3(copy_groups(c, B)), dim3(256), 0, stream, c, ws.copy_src, ws.copy_dst, ws.copies, 0);
   return launched();

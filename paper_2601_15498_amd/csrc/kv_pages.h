@@ -7,8 +7,7 @@
 namespace mars {
 namespace kv {
 
-constexpr int kPlanThreads = 1024;
-constexpr int kPlanWaves = kPlanThreads / kWave;
+constexpr int kPlanFew = 256, kPlanMany = 1024;  // threads of the work-group that plans a reserve: a barrier of four waves is the quicker one
 
 // Workspace of a reserve: the pages found, the copies to make.
 struct ReserveSpace {
@@ -18,7 +17,7 @@ struct ReserveSpace {
 };
 constexpr int kCopyBit = 1 << 30;  // of the pages a request wants: the first is to be a copy of the one it shares
 // Sum of v over the threads in front of this one, and over all.
-__device__ __forceinline__ int scan(int v, int* sh, int& total) {
+template <int THREADS> __device__ __forceinline__ int scan(int v, int* sh, int& total) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   int x = v;
 #pragma unroll
@@ -32,7 +31,7 @@ __device__ __forceinline__ int scan(int v, int* sh, int& total) {
   int front = 0;
   total = 0;
 #pragma unroll
-  for (int w = 0; w < kPlanWaves; ++w) {
+  for (int w = 0; w < THREADS / kWave; ++w) {
     if (w < wave) front += sh[w];
     total += sh[w];
   }
@@ -41,18 +40,20 @@ __device__ __forceinline__ int scan(int v, int* sh, int& total) {
 
 // One work-group: requests' wants, the lowest free pages, the tables.  What it knows of the requests lies in LDS.
 // What bounds it: the latency of its chain of loads (sequence, length, page, count) and barriers, and the way through refs to the free
-// pages, 16 384 of them per step.
-__global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Cache c, const int32_t* __restrict__ seqs, const int32_t* __restrict__ n_new,
+// pages, 16 of them per thread and step.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) reserve_kernel(Cache c, const int32_t* __restrict__ seqs, const int32_t* __restrict__ n_new,
                                                                int B, int N, int32_t* __restrict__ status, ReserveSpace ws) {
-  __shared__ int sh[kPlanWaves];
-  __shared__ __attribute__((aligned(16))) int sh_shared[MARS_KV_MAX_REQUESTS + 3];
-  __shared__ int sh_seq[MARS_KV_MAX_REQUESTS], sh_held[MARS_KV_MAX_REQUESTS], sh_wants[MARS_KV_MAX_REQUESTS], sh_begin[MARS_KV_MAX_REQUESTS];
-  __shared__ uint8_t sh_why[MARS_KV_MAX_REQUESTS];
+  constexpr int MOST = THREADS == kPlanFew ? kPlanFew : MARS_KV_MAX_REQUESTS;
+  __shared__ int sh[THREADS / kWave];
+  __shared__ __attribute__((aligned(16))) int sh_shared[MOST + 3];
+  __shared__ int sh_seq[MOST], sh_held[MOST], sh_wants[MOST], sh_begin[MOST];
+  __shared__ uint8_t sh_why[MOST];
   const int tid = threadIdx.x, P = 1 << c.log_page;
 
   // what every request needs; the page its first new token goes to
   bool any = false;  // a page that others hold too
-  for (int b = tid; b < B; b += kPlanThreads) {
+  for (int b = tid; b < B; b += THREADS) {
     const int s = sequence_of(c, seqs, b);
     int shared = -1, wants = 0, held = 0, why = MARS_KV_OK;
     if (s < 0) {
@@ -78,7 +79,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Cache c, const in
   if (tid < 3) sh_shared[B + tid] = -1;
   // a page that others hold too is copied, unless this is the last of its holders and all of them are here
   if (__syncthreads_or(any)) {
-    for (int b = tid; b < B; b += kPlanThreads) {
+    for (int b = tid; b < B; b += THREADS) {
       const int mine = sh_shared[b], holders = mine >= 0 ? c.refs[mine] : 0;
       if (holders <= 1) continue;
       int here = 0, later = 0;
@@ -95,10 +96,10 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Cache c, const in
 
   // in order of the requests
   long demand = 0;
-  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+  for (int b0 = 0; b0 < B; b0 += THREADS) {
     const int b = b0 + tid;
     int total;
-    const int before = scan(b < B ? sh_wants[b] & ~kCopyBit : 0, sh, total);
+    const int before = scan<THREADS>(b < B ? sh_wants[b] & ~kCopyBit : 0, sh, total);
     if (b < B) sh_begin[b] = static_cast<int>(min(demand + before, 0x3FFFFFFFl));
     demand += total;
   }
@@ -106,7 +107,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Cache c, const in
   // the lowest free pages, as many as are wanted
   const int most = static_cast<int>(min(demand, static_cast<long>(c.pages)));
   int have = 0;
-  for (int p0 = 0; p0 < c.pages && have < most; p0 += kPlanThreads * 16) {
+  for (int p0 = 0; p0 < c.pages && have < most; p0 += THREADS * 16) {
     const int p = p0 + tid * 16;
     u32 free = 0;
     if (p + 16 <= c.pages && reinterpret_cast<uintptr_t>(c.refs) % 16 == 0) {
@@ -122,7 +123,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Cache c, const in
         if (p + i < c.pages && c.refs[p + i] == 0) free |= 1u << i;
     }
     int total;
-    int at = have + scan(__popc(free), sh, total);
+    int at = have + scan<THREADS>(__popc(free), sh, total);
     while (free && at < most) {
       ws.found[at++] = p + __ffs(free) - 1;
       free &= free - 1;
@@ -134,12 +135,12 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Cache c, const in
 
   // A request that does not get all it wants gets nothing; begin only grows, so those behind it that want any get nothing either.
   int copies = 0;  // those in front, the same in all threads
-  for (int b0 = 0; b0 < B; b0 += kPlanThreads) {
+  for (int b0 = 0; b0 < B; b0 += THREADS) {
     const int b = b0 + tid;
     const int want = b < B ? sh_wants[b] & ~kCopyBit : 0;
     const bool fits = b < B && sh_begin[b] + want <= have, copy = fits && (sh_wants[b] & kCopyBit);
     int total;
-    const int rank = copies + scan(copy, sh, total);
+    const int rank = copies + scan<THREADS>(copy, sh, total);
     copies += total;
     if (b < B && want) {
       if (!fits) {
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Cache c, const in
   }
   if (tid == 0) *ws.copies = copies;
   // the pages that are added: a thread per page, which looks its request up
-  for (int k = tid; k < have; k += kPlanThreads) {
+  for (int k = tid; k < have; k += THREADS) {
     int lo = 0, hi = B - 1;  // the last request that begins at k or before; those that want none come before it or begin later
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -176,7 +177,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_kernel(Cache c, const in
   // The last holder of a page keeps it only if the others got their copies (the counts are read past the first cache, where the
   // subtractions above were made).
   __syncthreads();
-  for (int b = tid; status && b < B; b += kPlanThreads) {
+  for (int b = tid; status && b < B; b += THREADS) {
     int why = sh_why[b];
     if (sh_shared[b] >= 0 && !(sh_wants[b] & kCopyBit) && why == MARS_KV_OK &&
         __hip_atomic_load(&c.refs[sh_shared[b]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 1)
