@@ -63,43 +63,42 @@ constexpr int kPlanFewPages = 16384;  // four steps of the search
 
 // ---------------------------------------------------------------- attention: how the work is laid out
 struct AttnPlan {
-  int mode, blocks_rb;  // waves divide keys or rows; blocks of 16 rows per wave
-  int nodes;            // of a block of rows
-  u32 groups;           // work-groups beside each other on the chip
-  size_t bytes;         // of pieces
+  int mode, rows;  // waves divide keys or rows; rows of a wave
+  int waves;       // of a work-group
+  int nodes;       // of a block of rows
+  u32 groups;      // work-groups beside each other on the chip
+  size_t bytes;    // of pieces
 };
-static size_t piece_bytes(int dim, int rb) { return sizeof(float) * (32 * rb + static_cast<size_t>(rb) * (dim / 16) * 256); }
-
+// Up to 32 rows of bf16 the waves divide the keys: 28 rows over 4 caches of 60 000 - 131 000 tokens take 110 us so, and 165 in blocks of 16.  Beyond, 32
+// rows each, by 8 waves where their blocks hold no more rows than those of 4 (208 rows over long caches: 440 us, by 4 waves 510; but 288 rows over 16
+// caches of 1 024 - 8 191: 181 and 170; 100 rows: 90 and 78).
+// In 32 bits the products take three times as long and 32 rows a third more registers: up to 64 rows 16 at a time are faster (48 rows: 48 us instead of 78;
+// 120 rows: 98 instead of 92).
 static AttnPlan attn_plan(int N, int group, int dim, int dtype) {
   const long rows = static_cast<long>(N) * group;
+  const bool f32 = dtype == MARS_F32;
   AttnPlan p;
-  p.mode = KEYS;
-  if (dtype == MARS_F32) {
-    p.blocks_rb = 1;
-    if (rows > 16) p.mode = ROWS;
-  } else if (rows <= 16) {
-    p.blocks_rb = 1;
-  } else if (rows <= 32) {
-    p.blocks_rb = 2;
-  } else {
-    p.blocks_rb = 2;
-    p.mode = ROWS;
-  }
-  p.groups = 256 * per_unit(dim, p.blocks_rb, dtype == MARS_F32);
-  p.nodes = (p.mode == ROWS ? 64 : 16) * p.blocks_rb / group;
-  p.bytes = align_up(static_cast<size_t>(p.groups) * 2 * (p.mode == ROWS ? 4 : 1) * piece_bytes(dim, p.blocks_rb));
+  p.mode = (f32 ? group <= 16 && rows <= 64 : rows <= 32) ? KEYS : ROWS;
+  p.rows = p.mode == KEYS && (f32 || rows <= 16) ? 16 : 32;
+  const long four = (rows + kWaves * 32 - 1) / (kWaves * 32);  // blocks of four waves
+  p.waves = p.mode == ROWS && four % 2 == 0 && !f32 && dim <= 128 ? 2 * kWaves : kWaves;
+  p.groups = 256 * per_unit(dim, p.mode, p.waves, p.rows, f32);
+  p.nodes = (p.mode == ROWS ? p.waves * p.rows : p.rows) / group;
+  // (a wave's piece: its rows' references and sums, and its results)
+  const size_t piece = sizeof(float) * (2 * p.rows + static_cast<size_t>(p.rows) * dim);
+  p.bytes = align_up(static_cast<size_t>(p.groups) * 2 * (p.mode == ROWS ? p.waves : 1) * piece);
   return p;
 }
 // Blocks of so few units (as far as the caller says) are not cut: their pieces would have to be joined by a second kernel.
 constexpr int kWholeUnits = 8;
-constexpr int kMergeRows = 4;
 
-template <int D, int RB, typename T, int MODE> static int launch_attention(u32 groups, const AttnArgs& a, hipStream_t stream) {
-  if (a.c.log_page >= 5) hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE, true>), dim3(groups), dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL((attention_kernel<D, RB, T, MODE, false>), dim3(groups), dim3(kThreads), 0, stream, a);
+template <typename W> static int launch_attention(u32 groups, const AttnArgs& a, hipStream_t stream) {
+  static_assert(Piece<W>::kFloats == 2 * W::kRows + W::kRows * W::D, "as attn_plan counts them");
+  if (a.c.log_page >= 5) hipLaunchKernelGGL((attention_kernel<W, true>), dim3(groups), dim3(W::kGroupWaves * kWave), 0, stream, a);
+  else hipLaunchKernelGGL((attention_kernel<W, false>), dim3(groups), dim3(W::kGroupWaves * kWave), 0, stream, a);
   if (hipGetLastError() != hipSuccess) return MARS_ERR_HIP;
   if (a.whole) return MARS_OK;
-  hipLaunchKernelGGL((merge_kernel<D, RB, T, MODE>), dim3(groups - 1, MODE == ROWS ? kMergeRows : RB), dim3(kThreads), 0, stream, a, groups);
+  hipLaunchKernelGGL(merge_kernel<W>, dim3(groups - 1, W::kStrips), dim3(kThreads), 0, stream, a, groups);
   return launched();
 }
 
@@ -220,9 +219,14 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   return by_dim(cache->dim, [&](auto dim) {
     constexpr int D = decltype(dim)::value;
-    if (dtype == MARS_F32) return p.mode == KEYS ? launch_attention<D, 1, float, KEYS>(groups, a, stream) : launch_attention<D, 1, float, ROWS>(groups, a, stream);
-    if (p.mode == ROWS) return launch_attention<D, 2, bf16_t, ROWS>(groups, a, stream);
-    return p.blocks_rb == 1 ? launch_attention<D, 1, bf16_t, KEYS>(groups, a, stream) : launch_attention<D, 2, bf16_t, KEYS>(groups, a, stream);
+    if (p.mode == KEYS) {
+      if (dtype == MARS_F32) return launch_attention<Narrow<D, 1, float>>(groups, a, stream);
+      return p.rows == 16 ? launch_attention<Narrow<D, 1, bf16_t>>(groups, a, stream) : launch_attention<Narrow<D, 2, bf16_t>>(groups, a, stream);
+    }
+    if (dtype == MARS_F32) return launch_attention<Wide<D, float, kWaves>>(groups, a, stream);
+    if constexpr (D <= 128)
+      if (p.waves > kWaves) return launch_attention<Wide<D, bf16_t, 2 * kWaves>>(groups, a, stream);
+    return launch_attention<Wide<D, bf16_t, kWaves>>(groups, a, stream);
   });
 }
 

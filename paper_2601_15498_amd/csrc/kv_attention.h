@@ -1,70 +1,38 @@
 // Attention of a step's nodes over the paged 4-bit cache (include/mars_cache.h):
 //   o = sum_j p_j v_j / sum_j p_j,   p_j = exp2(c s_j - m),   s_j = q . k_j,   c = scale * log2(e),
-// one pass over the keys with a running reference m and sum.
+// one pass over the keys with a running reference m and sum.  A wave takes tiles of 32 keys, whose codes come through a ring in LDS (kv_tiles.h).  The
+// keys, then the values, are the first operand of the two products, so that a lane has the scores of one query row, and the order of the keys
+// and channels inside the products, which is free, is chosen so that the probabilities are the second product's second operand in the registers they are
+// formed in.  A conversion of codes to bf16 is exact; it gives two channels of one key where the second product takes two keys of one channel: a
+// byte permutation per two values.
 //
-// A wave takes 16 RB query rows (nodes x query heads of one cache head) and tiles of 32 keys.  Both products run on
-// v_mfma_f32_16x16x32_bf16 with the keys, then the values, as the first operand, straight from the packed codes in registers:
-// no LDS and no barrier on the way, and the probabilities never leave the registers they are formed in.
-//   scores    first operand: lane (r = l%16, g = l/16) holds row r of a block of 16 keys, a quarter (D/4) of its channels, which is
-//             contiguous in the page, with one scale (D = 256: two).  The order of the channels inside the product is free, so the queries are loaded
-//             to match.  Row 4g + i of block b is the tile's key 8g + 4b + i, so that a lane ends up with the scores of the eight
-//             keys 8g .. 8g + 7 for its query, in order --
-//   values    -- which is what the second product's second operand holds.  Its first one: lane (r, g) has eight keys 8g .. 8g + 7 of D/16
-//             channels of its own, in the page contiguous as well (that is what the values' layout is for).  A conversion gives two
-//             channels of one key, the product takes two keys of one channel: a byte permutation per two values in between.
-// The conversions are exact (a code times a power of two is a bf16 value).
-//
-// Few rows: the four waves of a work-group take every fourth tile of the same rows and meet in LDS at the end (KEYS).  Many: each
-// wave has rows of its own (ROWS).  The work -- all tiles of all (request, cache head, block of rows) items -- is dealt out evenly: a
-// work-group takes a run of tiles that may begin and end inside an item; what it has of such an item goes to the workspace, and
-// merge_kernel joins the pieces.  Every work-group works out the deal from the lengths by itself.
+// Few rows (Narrow, up to 32): the four waves of a work-group take every fourth tile of the same rows and meet in LDS at the end.  Bound by the cache's way from
+// memory: 64 tokens over 500 - 8 192, 304 MB, 73 us, of which in the middle 8.5 TB/s, the rest is the beginning and the end.
+// More (Wide): each of four or eight waves has 32 rows of its own, the values are converted once for all of them.  Bound by what the card may draw: the matrix cores
+// work for half of the clocks, at 1.7 to 2.0 GHz.
+// The work is dealt out by kv_deal.h: a work-group takes a run of tiles that may begin and end inside a block of rows; what it has of such a
+// block goes to the workspace, and merge_kernel joins the pieces.
 #pragma once
 
 #include <type_traits>
+#include <utility>
 
+#include "kv_deal.h"
 #include "kv_format.h"
 #include "kv_rows.h"
+#include "kv_tiles.h"
 
 namespace mars {
 namespace kv {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
-constexpr int kTile = 32;             // keys per wave and step
-constexpr int kUnit = kWaves * kTile; // keys of a unit of work: each wave fetches a tile of it
 constexpr float kFloor = -3.0e38f;    // the reference before the first key that counts
 constexpr float kSlack = 8.0f;        // how far (in powers of two) scores may pass the reference before it is moved up
-
-struct AttnArgs {
-  Cache c;
-  size_t layer_offset;
-  const int32_t* seqs;
-  const int32_t* n_new;
-  const unsigned long long* mask;
-  const void* q;
-  long q_request, q_node, q_head;
-  void* out;
-  long out_request, out_node, out_head;
-  float* lse;
-  float* partial;
-  float scale_log2;
-  int B, N, q_heads, group, words;
-  int nodes;    // of a block of rows
-  bool whole;   // the deal gives out whole items
-};
+enum { KEYS = 0, ROWS = 1 };          // what the waves of a work-group divide between them
 
 __device__ __forceinline__ float max3(float a, float b, float c) {  // (written out: fmaxf would first quiet each operand)
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
-}
-__device__ __forceinline__ float over_groups_max(float v) {  // over the four lanes that share l % 16
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
-}
-__device__ __forceinline__ float over_groups_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
 }
 __device__ __forceinline__ bf16x8 as_bf16x8(u32 a, u32 b, u32 c, u32 d) { return __builtin_bit_cast(bf16x8, u32x4{a, b, c, d}); }
 __device__ __forceinline__ u32 round_pair(float a, float b) { return __builtin_bit_cast(u32, __builtin_convertvector(f32x2{a, b}, bf16x2)); }
@@ -83,284 +51,101 @@ template <int TERMS> __device__ __forceinline__ void split_pair(float a, float b
   }
 }
 
-// ---------------------------------------------------------------- the deal
-// A request's items are (cache head, block of `nodes` nodes), its units those of its items.  Under a mask a block has all the request's keys.
-// In a chain it has those up to its last node, and blocks are taken in pairs, the last with the first and so on, so that every pair has about
-// the same number of units: `per`, which is rounded up (what is left over of it is idle).
-struct Request {
-  int n, len, blocks, pairs;  // pairs: of blocks, or blocks
-  u32 per;                    // units of a pair, or of a block
-  __device__ __forceinline__ Request() {}
-  __device__ __forceinline__ Request(const AttnArgs& a, int b) {
-    const int s = sequence_of(a.c, a.seqs, b);
-    n = a.n_new ? min(max(a.n_new[b], 0), a.N) : a.N;
-    len = 0;
-    if (s >= 0) len = min(max(a.c.lens[s], 0), a.c.width << a.c.log_page);
-    else n = 0;
-    blocks = (n + a.nodes - 1) / a.nodes;
-    const bool paired = !a.mask && blocks > 1;
-    pairs = paired ? (blocks + 1) / 2 : blocks;
-    per = paired ? (2u * len + static_cast<u32>(blocks + 1) * a.nodes + 2 * (kUnit - 1)) / kUnit : static_cast<u32>(len + n + kUnit - 1) / kUnit;
-  }
-  __device__ __forceinline__ u32 items(const AttnArgs& a) const { return static_cast<u32>(a.c.heads) * pairs; }
-  // Keys that a block's rows see at most.
-  __device__ __forceinline__ int keys(const AttnArgs& a, int block) const { return len + (a.mask ? n : min(n, (block + 1) * a.nodes)); }
-  __device__ __forceinline__ u32 block_units(const AttnArgs& a, int block) const { return static_cast<u32>(keys(a, block) + kUnit - 1) / kUnit; }
-};
-// Over the wave's lanes, lane 0 first: inside each row of 16 by shifts, then the rows in front through scalar registers (a scan by exchanges
-// through LDS took a microsecond of every launch).  A lane whose source falls outside its row gets 0.
-__device__ __forceinline__ u32 wave_scan(u32 v) {
-  v += dpp<0x111>(v);  // row_shr 1, 2, 4, 8
-  v += dpp<0x112>(v);
-  v += dpp<0x114>(v);
-  v += dpp<0x118>(v);
-  const u32 t0 = __builtin_amdgcn_readlane(v, 15), t1 = __builtin_amdgcn_readlane(v, 31), t2 = __builtin_amdgcn_readlane(v, 47);
-  const u32 row = threadIdx.x % kWave / 16;
-  return v + (row > 0 ? t0 : 0) + (row > 1 ? t1 : 0) + (row > 2 ? t2 : 0);
-}
-__device__ __forceinline__ u32 wave_sum(u32 v) { return __builtin_amdgcn_readlane(wave_scan(v), kWave - 1); }
-__device__ __forceinline__ u32 wave_max(u32 v) {
-  v = max(v, dpp<0x111>(v));
-  v = max(v, dpp<0x112>(v));
-  v = max(v, dpp<0x114>(v));
-  v = max(v, dpp<0x118>(v));
-  return max(max(static_cast<u32>(__builtin_amdgcn_readlane(v, 15)), static_cast<u32>(__builtin_amdgcn_readlane(v, 31))),
-             max(static_cast<u32>(__builtin_amdgcn_readlane(v, 47)), static_cast<u32>(__builtin_amdgcn_readlane(v, 63))));
-}
-// What a work-group's share of the units comes to, and a place in the deal, kept by every wave for itself: 64 requests at a time, one per lane.
-// Where no work-group gets much more by it (kJoinCost), whole items are given out and none is cut: then an item counts as two, one for each
-// of its blocks.
-constexpr u32 kJoinCost = 8;  // units; two prompts of 2 048, every pair of blocks with a work-group of its own: 50 units instead of 45, and the
-                              // pieces' 134 MB neither written nor read
-struct Deal {
-  const AttnArgs& a;
-  Request mine;       // of request first + lane
-  int first;
-  u32 front, before;  // units in front of the 64, in front of the lane's request
-  u32 sum;            // of the 64
-  u32 total, share;
-  bool whole;
-  __device__ __forceinline__ u32 units(const Request& r) const { return whole ? 2 * r.items(a) : r.items(a) * r.per; }
-  __device__ __forceinline__ void place(u32 units_in_front) {
-    front = units_in_front;
-    const u32 v = first + static_cast<int>(threadIdx.x % kWave) < a.B ? units(mine) : 0;
-    const u32 x = wave_scan(v);
-    before = front + x - v;
-    sum = __builtin_amdgcn_readlane(x, kWave - 1);
-  }
-  __device__ __forceinline__ void load(int b0) {
-    first = b0;
-    mine = Request(a, min(b0 + static_cast<int>(threadIdx.x % kWave), a.B - 1));
-  }
-  __device__ __forceinline__ Deal(const AttnArgs& args, u32 groups) : a(args) {
-    u32 items = 0, most = 0;
-    total = 0;
-    whole = false;
-    for (int b = a.B - 1 & ~(kWave - 1); b >= 0; b -= kWave) {  // (ends at the first 64)
-      load(b);
-      const bool in = b + static_cast<int>(threadIdx.x % kWave) < a.B;
-      items += wave_sum(in ? mine.items(a) : 0);
-      total += wave_sum(in ? mine.items(a) * mine.per : 0);
-      most = max(most, wave_max(in && mine.items(a) ? mine.per : 0));
-    }
-    share = (total + groups - 1) / groups;
-    const u32 each = (items + groups - 1) / groups;
-    whole = a.whole || each * most <= share + kJoinCost;
-    if (whole) {
-      share = 2 * each;
-      total = 2 * items;
-    }
-    place(0);
-  }
-  // The block that unit u (not before an earlier call's) belongs to.
-  struct Place {
-    int b, head, block;
-    u32 begin, count;   // of the block in the deal; count = 0: idle
-    u32 offset;         // of u in the block; of idle ones: how many there are from u on
-    Request r;
-  };
-  __device__ __forceinline__ Place find(u32 u) {
-    while (u >= front + sum) {  // (u < total: there are more)
-      load(first + kWave);
-      place(front + sum);
-    }
-    const unsigned long long at = __ballot(before <= u && first + static_cast<int>(threadIdx.x % kWave) < a.B);
-    // the last that begins at u or before; those without units that begin there too come before it or not at all
-    const int lane = 63 - __builtin_clzll(at);
-    Place p;
-    p.b = first + lane;
-    p.r.n = __builtin_amdgcn_readlane(mine.n, lane);
-    p.r.len = __builtin_amdgcn_readlane(mine.len, lane);
-    p.r.blocks = __builtin_amdgcn_readlane(mine.blocks, lane);
-    p.r.pairs = __builtin_amdgcn_readlane(mine.pairs, lane);
-    p.r.per = __builtin_amdgcn_readlane(mine.per, lane);
-    const u32 local = u - __builtin_amdgcn_readlane(before, lane), per = whole ? 2 : p.r.per;
-    const u32 item = local / per, in = local % per;
-    p.head = item / p.r.pairs;
-    p.block = item % p.r.pairs;
-    const bool paired = p.r.pairs != p.r.blocks;  // (one block alone is no pair)
-    const int late = paired ? p.r.blocks - 1 - p.block : p.block;
-    const u32 those = whole ? 1 : paired ? p.r.block_units(a, late) : per;
-    p.offset = in;
-    if (in < those) {
-      p.block = late;
-      p.count = those;
-    } else {
-      p.offset = in - those;
-      p.count = late == p.block ? 0 : whole ? 1 : p.r.block_units(a, p.block);
-      if (p.offset >= p.count) {
-        p.count = 0;
-        p.offset = per - in;
-      }
-    }
-    p.begin = u - p.offset;
-    return p;
-  }
-};
+// f(0), f(1), .. f(N - 1), each with its constant.
+template <int... I, typename F> __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, typename F> __device__ __forceinline__ void each(F f) { each_of(std::make_integer_sequence<int, N>{}, f); }
 
-// ---------------------------------------------------------------- tiles on their way through LDS
-// A tile of 32 keys in LDS: codes of the keys, codes of the values, then the scales of both.  Sixteen bytes go from memory to LDS per lane and
-// instruction, past the registers, to places that follow each other; which sixteen they are is chosen so that the reads below find
-// sixteen lanes' pieces on sixteen different groups of four banks.
-template <int D> struct Tile {
-  static constexpr int kCodes = 16 * D, kScales = D <= 128 ? 256 : 512;  // bytes
-  static constexpr int kBytes = 2 * kCodes + kScales;
-  static constexpr int kCodeLoads = kCodes / 1024, kScaleLoads = kScales / 256;
-  static constexpr int kLoads = 2 * kCodeLoads + kScaleLoads;
-  static constexpr int S = D / 32, VW = D == 256 ? 16 : 8;
-  // Where sixteen bytes of the keys' codes stand: piece p (of D/32) of token t.
-  __device__ static __forceinline__ u32 key_slot(u32 t, u32 p) {
-    if (D == 64) return (t ^ (t >> 1 & 4)) * 2 + (p ^ (t >> 4 & 1));
-    if (D == 128) return t * 4 + (p ^ (t >> 3 & 3));
-    return t * 8 + (p ^ (t >> 2 & 6) ^ (t >> 1 & 1));
-  }
-  // And which piece of which token stands at `slot`: offset in the page's codes (from the tile's first token on).
-  __device__ static __forceinline__ u32 key_source(u32 slot) {
-    if (D == 64) {
-      const u32 row = slot >> 1, t = row ^ (row >> 1 & 4);
-      return t * 32 + ((slot & 1) ^ (t >> 4 & 1)) * 16;
-    }
-    if (D == 128) {
-      const u32 t = slot >> 2;
-      return t * 64 + ((slot & 3) ^ (t >> 3 & 3)) * 16;
-    }
-    const u32 t = slot >> 3;
-    return t * 128 + ((slot & 7) ^ (t >> 2 & 6) ^ (t >> 1 & 1)) * 16;
-  }
-  // The same for the values: half h of dword column c (its eight tokens) of octet o.
-  __device__ static __forceinline__ u32 value_slot(u32 o, u32 c, u32 h) {
-    if (D == 64) return (o * 8 + c) * 2 + h;
-    if (D == 128) return (o * 16 + c) * 2 + (h ^ (c >> 3));
-    return (o * 16 + (c >> 1)) * 4 + ((((c & 1) << 1) | h) ^ (c >> 3));
-  }
-  __device__ static __forceinline__ u32 value_source(u32 slot) {
-    if (D == 64) return slot * 16;
-    if (D == 128) return (slot ^ (slot >> 4 & 1)) * 16;
-    return (slot ^ (slot >> 4 & 3)) * 16;
-  }
-};
-__device__ __forceinline__ u32 lds_address(const void* p) {
-  return static_cast<u32>(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p));
-}
-// To LDS from byte address `lds` on, lane after lane.  (Written by hand: behind the compiler's own form of these loads every read of
-// LDS waits for all that is in flight.  The wait states: a scalar operand can come from a vector instruction just before.)
-template <int BYTES> __device__ __forceinline__ void buffer_to_lds(__amdgpu_buffer_rsrc_t rows, u32 at, u32 base, u32 lds) {
-  if constexpr (BYTES == 16)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds), "v"(at), "s"(rows), "s"(base) : "memory", "m0");
-  else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(lds), "v"(at), "s"(rows), "s"(base) : "memory", "m0");
-}
-template <int BYTES> __device__ __forceinline__ void global_to_lds(const uint8_t* at, u32 lds) {
-  if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(at) : "memory", "m0");
-  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(at) : "memory", "m0");
-}
-template <int LEFT> __device__ __forceinline__ void arrived() {  // all loads of this wave but the last LEFT
-  static_assert(LEFT >= 0 && LEFT < 64, "the counter's range");
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
-}
-constexpr int kBufferFlags = 0x00020000;  // untyped buffer, 32-bit data format
+// Two keys' values of the same channel beside each other: the low halves of two conversions, or the high ones.
+__device__ __forceinline__ u32 low_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// Fetches a wave's tiles of one piece of work, unit after unit.  UNIFORM: pages of 32 tokens and more, so that a tile lies in one page (a
-// buffer, which the loads cannot leave).  Otherwise an octet does.  The page numbers of the next units lie in one register, a lane each: a load of the
-// compiler's own in every unit would be waited for together with all that is in flight.
-template <int D, bool UNIFORM> struct Fetch {
-  using X = Tile<D>;
-  static constexpr int kSpan = UNIFORM ? kWave : kWave / 4;  // units whose pages are known at a time
-  const AttnArgs& a;
-  const int32_t* row;  // of the page table
-  int head, end, t0;   // keys there are; the next tile's first
-  int ids, at;         // pages, which of them is next
-  __device__ __forceinline__ Fetch(const AttnArgs& a_, int s, int head_, int end_, int from)
-      : a(a_), row(a_.c.page_table + static_cast<size_t>(s) * a_.c.width), head(head_), end(end_), t0(from) {
-    look_up();
+// The queries, as the first product's second operand, are bf16 rows as they are; fp32 rows are three bf16 terms, as the probabilities then are (one term for bf16
+// rows, whose results are rounded to as many bits).  The matrix cores also take codes and scales as they are, by queries of 8 bits: two such terms hold a bf16 number,
+// and the conversion of the keys falls away (395 us instead of 440 with long caches, nothing with few rows).  But products of one instruction 2^16 below the
+// largest are dropped there, and scores of 100 came out 1e-3 off; so it is not used.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// Which of the keys first .. first + 7 (numbered from the first node on; committed ones are < 0) row `node` of n nodes sees.  `only`: its mask, if that
+// is one word.
+__device__ __forceinline__ u32 seen(const AttnArgs& a, unsigned long long only, int b, int node, int n, int first) {
+  u32 bits;
+  if (a.mask) {
+    const unsigned long long* row = a.mask + (static_cast<size_t>(b) * a.N + node) * a.words;
+    auto word = [&](int w) { return w < 0 ? ~0ull : w >= a.words ? 0ull : a.words == 1 ? only : row[w]; };
+    const int w = first >> 6, shift = first & 63;
+    bits = static_cast<u32>(word(w) >> shift);
+    if (shift > 56) bits |= static_cast<u32>(word(w + 1) << (64 - shift));
+  } else {
+    const int k = node + 1 - first;
+    bits = k >= 8 ? 0xFFu : k <= 0 ? 0u : (1u << k) - 1;
   }
-  // (past the end: the last position's page; -1 past the table)
-  __device__ __forceinline__ void look_up() {
-    const int lane = threadIdx.x % kWave, t = UNIFORM ? t0 + lane * kUnit : t0 + lane / 4 * kUnit + lane % 4 * 8;
-    const int i = min(t, end - 1) >> a.c.log_page;
-    ids = i < a.c.width ? row[i] : -1;
-    asm volatile("" : "+v"(ids));  // waited for here, and not wherever it is next read
-    at = 0;
-  }
-  // Octet (of the tile's four) that a lane's share of load i of the codes, or of the scales, belongs to.
-  __device__ static __forceinline__ int code_octet(int i) { return (i * kWave + static_cast<int>(threadIdx.x % kWave)) / (D / 4); }
-  __device__ static __forceinline__ int scale_octet() {
-    const int lane = threadIdx.x % kWave;
-    return D == 256 ? lane / 16 : D == 128 ? lane % 32 / 8 : lane % 16 / 4;
-  }
-  // The next tile to LDS.  Returns which of its octets have no page (bit by bit).
-  __device__ __forceinline__ u32 next(u32 lds) {
-    if (at == kSpan) look_up();
-    const u32 lane = threadIdx.x % kWave, lp = a.c.log_page, in_page = (1u << lp) - 1;
-    u32 bad;
-    if constexpr (UNIFORM) {
-      const u32 id = __builtin_amdgcn_readlane(ids, at);
-      bad = id >= static_cast<u32>(a.c.pages) ? 0xF : 0;
-      const auto rows = __builtin_amdgcn_make_buffer_rsrc(head_of(a.c, a.layer_offset, bad ? 0 : id, head), 0, static_cast<int>(a.c.blk), kBufferFlags);
-      const u32 t = static_cast<u32>(t0) & in_page, k0 = t * (D / 2), v0 = ((D / 2) << lp) + k0;
-#pragma unroll
-      for (int i = 0; i < X::kCodeLoads; ++i) buffer_to_lds<16>(rows, X::key_source(i * kWave + lane), k0, lds + i * 1024);
-#pragma unroll
-      for (int i = 0; i < X::kCodeLoads; ++i) buffer_to_lds<16>(rows, X::value_source(i * kWave + lane), v0, lds + X::kCodes + i * 1024);
-      const u32 s0 = (D << lp) + t * (D / 32), of_values = (D / 32) << lp;
-      if constexpr (D == 256) {
-        buffer_to_lds<4>(rows, lane * 4, s0, lds + 2 * X::kCodes);
-        buffer_to_lds<4>(rows, lane * 4, s0 + of_values, lds + 2 * X::kCodes + 256);
-      } else {  // the keys' scales in lanes 0 .. 31 (D = 64: twice), the values' in the others
-        buffer_to_lds<4>(rows, lane % (D / 4) * 4 + lane / 32 * of_values, s0, lds + 2 * X::kCodes);
-      }
-    } else {
-      bad = __ballot(static_cast<u32>(ids) >= static_cast<u32>(a.c.pages)) >> (at * 4) & 0xF;
-      const u32 last = static_cast<u32>(end - 1) & ~7u;  // (octets past the end: the last one's place)
-      auto head_at = [&](int octet) {
-        const int p = __shfl(ids, at * 4 + octet);
-        return head_of(a.c, a.layer_offset, static_cast<u32>(p) < static_cast<u32>(a.c.pages) ? p : 0, head);
-      };
-#pragma unroll
-      for (int i = 0; i < X::kCodeLoads; ++i) {
-        const u32 o = code_octet(i), t = min(static_cast<u32>(t0) + 8 * o, last) & in_page;
-        const uint8_t* at = head_at(o) + t * (D / 2) - o * (4 * D);
-        global_to_lds<16>(at + X::key_source(i * kWave + lane), lds + i * 1024);
-        global_to_lds<16>(at + ((D / 2) << lp) + X::value_source(i * kWave + lane), lds + X::kCodes + i * 1024);
-      }
-      const u32 o = scale_octet(), t = min(static_cast<u32>(t0) + 8 * o, last) & in_page;
-      const uint8_t* scales = head_at(o) + (D << lp) + t * (D / 32) + lane % (D / 16) * 4;
-      if constexpr (D == 256) {
-        global_to_lds<4>(scales, lds + 2 * X::kCodes);
-        global_to_lds<4>(scales + ((D / 32) << lp), lds + 2 * X::kCodes + 256);
-      } else {
-        global_to_lds<4>(scales + (lane >= 32 ? (D / 32) << lp : 0), lds + 2 * X::kCodes);
-      }
-    }
-    t0 += kUnit;
-    ++at;
-    return bad;
+  const int k = n - first;
+  return bits & (k >= 8 ? 0xFFu : k <= 0 ? 0u : (1u << k) - 1);
+}
+
+// log of the sum of exponentials that l counts against the reference m.
+__device__ __forceinline__ float log_sum(float m, float l) { return l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f; }
+
+// A row of the block of nodes from node0 on: the `row`-th of `rows`, node by node, a cache head's query heads beside each other.
+template <typename T> struct RowOf {
+  int node, head;            // node < 0: there is no such row
+  unsigned long long word;   // its mask, where that is one word
+  const T* q;                // (where there is no row: the block's first)
+  __device__ __forceinline__ RowOf(const AttnArgs& a, int b, int cache_head, int node0, int row, int rows) {
+    const bool live = row < rows;
+    const int in = live ? row / a.group : 0;
+    node = node0 + in;
+    head = cache_head * a.group + (live ? row - in * a.group : 0);
+    word = a.mask && a.words == 1 ? a.mask[static_cast<size_t>(b) * a.N + node] : 0;
+    q = static_cast<const T*>(a.q) + b * a.q_request + static_cast<long>(node) * a.q_node + static_cast<long>(head) * a.q_head;
+    if (!live) node = -1;
   }
 };
+// Where the results of a lane go: element [f][i] of its row among the 16 from `row0` on is channel (4g + i) * D/16 + f0 + f.
+template <int D, int F, typename T>
+__device__ __forceinline__ void write_narrow(const AttnArgs& a, int b, int head, int node0, int row0, int rows, int f0, const f32x4 (&o)[F], float m, float l) {
+  constexpr int C = D / 16;
+  const int lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
+  const int row = row0 + r;
+  if (row >= rows) return;
+  const int in = row / a.group, node = node0 + in, h = head * a.group + row - in * a.group;
+  const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+  T* at = static_cast<T*>(a.out) + b * a.out_request + node * a.out_node + h * a.out_head + g * (4 * C) + f0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float x[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) x[f] = o[f][i] * inverse;
+    if constexpr (std::is_same<T, float>::value) {
+      if constexpr (F == 1) at[i * C] = x[0];
+      else if constexpr (F == 2) *reinterpret_cast<f32x2*>(at + i * C) = f32x2{x[0], x[1]};
+      else
+#pragma unroll
+        for (int f = 0; f < F; f += 4) *reinterpret_cast<f32x4*>(at + i * C + f) = f32x4{x[f], x[f + 1], x[f + 2], x[f + 3]};
+    } else {
+      if constexpr (F == 1) at[i * C] = static_cast<bf16_t>(round_pair(x[0], 0.0f));
+      else if constexpr (F == 2) *reinterpret_cast<u32*>(at + i * C) = round_pair(x[0], x[1]);
+      else if constexpr (F == 4) *reinterpret_cast<u32x2*>(at + i * C) = u32x2{round_pair(x[0], x[1]), round_pair(x[2], x[3])};
+      else
+#pragma unroll
+        for (int f = 0; f < F; f += 8)
+          *reinterpret_cast<u32x4*>(at + i * C + f) = u32x4{round_pair(x[f], x[f + 1]), round_pair(x[f + 2], x[f + 3]),
+                                                            round_pair(x[f + 4], x[f + 5]), round_pair(x[f + 6], x[f + 7])};
+    }
+  }
+  if (a.lse && g == 0 && f0 == 0)
+    a.lse[(static_cast<size_t>(b) * a.N + node) * a.q_heads + h] = log_sum(m, l);
+}
+
+// ---------------------------------------------------------------- 16 rows per lane column
+// Both products on v_mfma_f32_16x16x32_bf16.  Lane (r = l % 16, g = l / 16):
+//   scores    first operand: row r of a block of 16 keys, a quarter of its channels.  Row 4g + i of block b is the tile's key 8g + 4b + i, so that the lane
+//             ends up with the scores of the eight keys 8g .. 8g + 7 for its query, in order --
+//   values    -- which is what the second product's second operand holds.  Its first one: eight keys 8g .. 8g + 7 of D/16 channels of its own.
 // What a lane has of a tile, in registers: sixteen keys' quarter twice, and eight keys' values.
-template <int D> struct Keys {
+template <int D> struct Keys16 {
   u32 k[2][D / 32], ks[2];
-  __device__ __forceinline__ explicit Keys(const uint8_t* tile) {
+  __device__ __forceinline__ explicit Keys16(const uint8_t* tile) {
     using X = Tile<D>;
     const u32 lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
     const uint8_t* scales = tile + 2 * X::kCodes;
@@ -384,14 +169,10 @@ template <int D> struct Keys {
     }
   }
 };
-// Two keys' values of the same channel beside each other: the low halves of two conversions, or the high ones.
-__device__ __forceinline__ u32 low_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
-__device__ __forceinline__ u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-
-template <int D> struct Values {
+template <int D> struct Values16 {
   u32 v[Tile<D>::VW];
   u32x2 vs;
-  __device__ __forceinline__ explicit Values(const uint8_t* tile) {
+  __device__ __forceinline__ explicit Values16(const uint8_t* tile) {
     using X = Tile<D>;
     const u32 lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
 #pragma unroll
@@ -436,18 +217,7 @@ template <int D> struct Values {
   }
 };
 
-// ---------------------------------------------------------------- a wave's rows
-// The queries as the first product's second operand.  Three forms:
-//   bf16 rows, D >= 128 (CODES): the keys' codes and scales go into the product as they are (4 bits by 8 bits, a scale per 32 channels), 128 channels at a time;
-//     the queries go in as two 8-bit terms of four significant bits each, which is all that a bf16 number has, with one scale per row: what is lost of a
-//     channel is below 2^-22 of the row's largest.  (The keys converted to bf16 instead: a third of the vector instructions that do not depend on the number of rows.)
-//   bf16 rows, D = 64: keys converted to bf16, 32 channels at a time.
-//   fp32 rows: the same with three bf16 terms.
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-template <int D, typename T> constexpr bool kCodes = D >= 128 && !std::is_same<T, float>::value;
-
-template <int D, int RB, typename T, bool CODES> struct Queries;
-template <int D, int RB, typename T> struct Queries<D, RB, T, false> {
+template <int D, int RB, typename T> struct Queries16 {
   static constexpr int S = D / 32, TERMS = std::is_same<T, float>::value ? 3 : 1;
   bf16x8 q[TERMS][RB][S];
   // Channels that lane group g takes in step s: eight from here on.
@@ -464,7 +234,7 @@ template <int D, int RB, typename T> struct Queries<D, RB, T, false> {
       for (int k = 0; k < TERMS; ++k) q[k][rb][s] = as_bf16x8(t[0][k], t[1][k], t[2][k], t[3][k]);
     }
   }
-  __device__ __forceinline__ void scores(const Keys<D>& x, f32x4 (&sc)[2][RB]) const {
+  __device__ __forceinline__ void scores(const Keys16<D>& x, f32x4 (&sc)[2][RB]) const {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
@@ -482,68 +252,15 @@ template <int D, int RB, typename T> struct Queries<D, RB, T, false> {
     }
   }
 };
-template <int D, int RB, typename T> struct Queries<D, RB, T, true> {
-  static constexpr int H = D / 128;
-  i32x8 q[2][RB][H];
-  int scale[2][RB];  // of the row's two terms, as bytes like the keys'
-  __device__ __forceinline__ void load(int rb, const T* row, bool live) {
-    // The 8-bit operand's lane group g has channels 16 g .. + 15 and 64 + 16 g .. + 15 of each 128.
-    const int g = threadIdx.x % kWave / 16;
-    Eight e[H][4];
-    u32 top = 0;
-#pragma unroll
-    for (int h = 0; h < H; ++h)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        e[h][i] = load_eight(row + h * 128 + i / 2 * 64 + g * 16 + i % 2 * 8);
-        top = max(top, top_bits(e[h][i]));
-      }
-    top = live ? top : 0;
-    top = max(top, static_cast<u32>(__shfl_xor(static_cast<int>(top), 16)));
-    top = max(top, static_cast<u32>(__shfl_xor(static_cast<int>(top), 32)));
-    // The largest is 128 to 256 of the first term's steps; the second's are 32 times finer (what the first leaves is at most 8 of its own).
-    const u32 exponent = max(top >> 23, 13u);
-    const bool bad = top >= 0x7F800000u;  // a query that is not finite: its scores are NaN
-    scale[0][rb] = bad ? 255 : static_cast<int>(exponent - 7);
-    scale[1][rb] = bad ? 255 : static_cast<int>(exponent - 12);
-    const float up = live ? __uint_as_float((261 - exponent) << 23) : 0.0f;  // 2^(7 - (exponent - 127))
-#pragma unroll
-    for (int h = 0; h < H; ++h)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float x0 = e[h][i].x[4 * j] * up, x1 = e[h][i].x[4 * j + 1] * up, x2 = e[h][i].x[4 * j + 2] * up, x3 = e[h][i].x[4 * j + 3] * up;
-          int first = __builtin_amdgcn_cvt_pk_fp8_f32(x0, x1, 0, false);
-          first = __builtin_amdgcn_cvt_pk_fp8_f32(x2, x3, first, true);
-          int second = __builtin_amdgcn_cvt_pk_fp8_f32((x0 - __builtin_amdgcn_cvt_f32_fp8(first, 0)) * 32.0f, (x1 - __builtin_amdgcn_cvt_f32_fp8(first, 1)) * 32.0f, 0, false);
-          second = __builtin_amdgcn_cvt_pk_fp8_f32((x2 - __builtin_amdgcn_cvt_f32_fp8(first, 2)) * 32.0f, (x3 - __builtin_amdgcn_cvt_f32_fp8(first, 3)) * 32.0f, second, true);
-          q[0][rb][h][2 * i + j] = first;
-          q[1][rb][h][2 * i + j] = second;
-        }
-  }
-  template <int H0> __device__ __forceinline__ f32x4 step(const Keys<D>& x, int b, int rb, f32x4 sc) const {
-    const i32x8 k = {static_cast<int>(x.k[b][4 * H0]), static_cast<int>(x.k[b][4 * H0 + 1]), static_cast<int>(x.k[b][4 * H0 + 2]), static_cast<int>(x.k[b][4 * H0 + 3]), 0, 0, 0, 0};
-    const int ks = static_cast<int>(x.ks[b]);
-    sc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q[1][rb][H0], sc, 4, 0, H0, ks, 0, scale[1][rb]);  // (4: codes of 4 bits, 0: of 8)
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q[0][rb][H0], sc, 4, 0, H0, ks, 0, scale[0][rb]);
-  }
-  __device__ __forceinline__ void scores(const Keys<D>& x, f32x4 (&sc)[2][RB]) const {
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        sc[b][rb] = step<0>(x, b, rb, f32x4{0, 0, 0, 0});
-        if constexpr (H == 2) sc[b][rb] = step<1>(x, b, rb, sc[b][rb]);
-      }
-  }
-};
-
-template <int D, int RB, typename T> struct Wave {
+template <int D_, int RB, typename T_> struct Narrow {
+  using T = T_;
+  using Keys = Keys16<D_>;
+  static constexpr int D = D_, MODE = KEYS, kRows = 16 * RB, kGroupWaves = kWaves;
   static constexpr int NF = D / 16;             // blocks of 16 channels of the result
+  static constexpr int kParts = RB * NF;        // of a wave's result, four numbers of a lane each
   static constexpr int TERMS = std::is_same<T, float>::value ? 3 : 1;
-  Queries<D, RB, T, kCodes<D, T>> q;
-  f32x4 o[NF][RB];
+  Queries16<D, RB, T> q;
+  f32x4 o[RB][NF];                              // [f][i]: channel (4g + i) D/16 + f
   float m[RB], l[RB];
   int node[RB];                                 // of this lane's rows; < 0: no row
   unsigned long long word[RB];                  // the row's mask, where it is one word
@@ -553,162 +270,470 @@ template <int D, int RB, typename T> struct Wave {
     const int r = threadIdx.x % 16;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      const int row = row0 + rb * 16 + r;
-      const bool live = row < rows;
-      const int in = live ? row / a.group : 0, h = live ? row - in * a.group : 0;
-      node[rb] = live ? node0 + in : -1;
-      word[rb] = a.mask && a.words == 1 ? a.mask[static_cast<size_t>(b) * a.N + node0 + in] : 0;
-      q.load(rb, static_cast<const T*>(a.q) + b * a.q_request + static_cast<long>(node0 + in) * a.q_node + static_cast<long>(head * a.group + h) * a.q_head, live);
+      const RowOf<T> row(a, b, head, node0, row0 + rb * 16 + r, rows);
+      node[rb] = row.node;
+      word[rb] = row.word;
+      q.load(rb, row.q, row.node >= 0);
       m[rb] = kFloor;
       l[rb] = 0.0f;
 #pragma unroll
-      for (int f = 0; f < NF; ++f) o[f][rb] = f32x4{0, 0, 0, 0};
+      for (int f = 0; f < NF; ++f) o[rb][f] = f32x4{0, 0, 0, 0};
     }
+  }
+  // One tile.  `plain` (the same for the wave): every row sees all of it, and all of it is there.  Otherwise: request b has n nodes behind
+  // `len` tokens, the tile begins at t0; `bad`: which of its octets have no page.
+  __device__ __forceinline__ void tile(const AttnArgs& a, const uint8_t* at, bool plain, int b, int len, int n, int t0, u32 bad) {
+    const float c = a.scale_log2;
+    const int g = threadIdx.x % kWave / 16;
+    Values16<D> values(at);
+    f32x4 sc[2][RB];
+    q.scores(Keys16<D>(at), sc);
+    __builtin_amdgcn_sched_barrier(0);  // (the values' conversions would be brought up to here, and their results kept)
+    if (!plain) {
+      const int first = t0 + g * 8 - len;
+      const bool poison = bad >> g & 1;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const u32 sees = node[rb] < 0 ? 0u : seen(a, word[rb], b, node[rb], n, first);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float s = poison ? __builtin_nanf("") : sc[k][rb][i];
+            sc[k][rb][i] = sees >> (4 * k + i) & 1 ? s : -__builtin_inff();
+          }
+      }
+      values.cut(poison ? 0 : n - first);
+    }
+    float top[RB];
+    bool up = false;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      float t = max3(sc[0][rb][0], sc[0][rb][1], sc[0][rb][2]);
+      t = max3(t, sc[0][rb][3], sc[1][rb][0]);
+      t = max3(t, sc[1][rb][1], sc[1][rb][2]);
+      t = max3(t, sc[1][rb][3], t);
+      top[rb] = t * c;
+      up |= top[rb] > m[rb] + kSlack;
+    }
+    if (__any(up)) {  // seldom after the first tiles
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float t = fmaxf(top[rb], __shfl_xor(top[rb], 16));
+        t = fmaxf(m[rb], fmaxf(t, __shfl_xor(t, 32)));
+        const float shrink = __builtin_amdgcn_exp2f(m[rb] - t);
+        m[rb] = t;
+        l[rb] *= shrink;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) o[rb][f] *= shrink;
+      }
+    }
+    u32 p[TERMS][RB][4];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[h / 2][rb][h % 2 * 2], c, -m[rb]));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[h / 2][rb][h % 2 * 2 + 1], c, -m[rb]));
+        l[rb] += e0 + e1;
+        u32 t[TERMS];
+        split_pair<TERMS>(e0, e1, t);
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) p[k][rb][h] = t[k];
+      }
+    __builtin_amdgcn_sched_barrier(0);
+    values.each([&](int f, bf16x8 v) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int t = TERMS - 1; t >= 0; --t)
+          o[rb][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, as_bf16x8(p[t][rb][0], p[t][rb][1], p[t][rb][2], p[t][rb][3]), o[rb][f], 0, 0, 0);
+    });
+  }
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      l[rb] += __shfl_xor(l[rb], 16);
+      l[rb] += __shfl_xor(l[rb], 32);
+    }
+  }
+  // The four waves' results for the same rows to wave 0.  sh: room for two waves' results; sh_m, sh_l: [4][kRows].
+  __device__ __forceinline__ void join(f32x4* sh_o, float* sh_m, float* sh_l) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 16;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+      if (lane < 16) {
+        sh_m[wave * kRows + rb * 16 + r] = m[rb];
+        sh_l[wave * kRows + rb * 16 + r] = l[rb];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      float all = kFloor, sum = 0.0f;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) all = fmaxf(all, sh_m[v * kRows + rb * 16 + r]);
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) sum += sh_l[v * kRows + rb * 16 + r] * __builtin_amdgcn_exp2f(sh_m[v * kRows + rb * 16 + r] - all);
+      const float shrink = __builtin_amdgcn_exp2f(m[rb] - all);
+#pragma unroll
+      for (int f = 0; f < NF; ++f) o[rb][f] *= shrink;
+      m[rb] = all;
+      l[rb] = sum;
+    }
+    // waves 2 and 3 to 0 and 1, then 1 to 0
+#pragma unroll
+    for (int half = 2; half >= 1; half >>= 1) {
+      f32x4* const sh = sh_o + (wave & (half - 1)) * (kParts * kWave) + lane;
+      if (wave >= half && wave < 2 * half) {
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) sh[i * kWave] = o[i / NF][i % NF];
+      }
+      __syncthreads();
+      if (wave < half) {
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) o[i / NF][i % NF] += sh[i * kWave];
+      }
+      __syncthreads();
+    }
+  }
+  __device__ __forceinline__ void write(const AttnArgs& a, int b, int head, int node0, int row0, int rows) const {
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) write_narrow<D, NF, T>(a, b, head, node0, row0 + rb * 16, rows, 0, o[rb], m[rb], l[rb]);
+  }
+  template <typename P> __device__ __forceinline__ void save(const P& piece) const {
+    const int lane = threadIdx.x % kWave;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb)
+      if (lane < 16) {
+        piece.reference(rb * 16 + lane) = m[rb];
+        piece.sum(rb * 16 + lane) = l[rb];
+      }
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) piece.part(i, lane) = o[i / NF][i % NF];
+  }
+  // Joining pieces: kStrips times a wave takes a quarter of the parts of kStripRows rows.
+  static constexpr int kStrips = RB, kStripRows = 16, kQuarter = NF / 4;
+  __device__ static __forceinline__ int strip_row(int strip) { return strip * 16 + threadIdx.x % 16; }  // of the lane, in the wave's rows
+  __device__ static __forceinline__ int strip_wave(int) { return 0; }                                    // whose piece
+  __device__ static __forceinline__ int strip_part(int strip, int quarter, int i) { return strip * NF + quarter * kQuarter + i; }
+  __device__ static __forceinline__ void write_quarter(const AttnArgs& a, int b, int head, int node0, int strip, int rows, int quarter, const f32x4 (&x)[kQuarter],
+                                                       float m, float l) {
+    write_narrow<D, kQuarter, T>(a, b, head, node0, strip * 16, rows, quarter * kQuarter, x, m, l);
   }
 };
 
-// Which of the keys first .. first + 7 (numbered from the first node on; committed ones are < 0) row `node` of n nodes sees.  `only`: its mask, if that
-// is one word.
-__device__ __forceinline__ u32 seen(const AttnArgs& a, unsigned long long only, int b, int node, int n, int first) {
-  u32 bits;
-  if (a.mask) {
-    const unsigned long long* row = a.mask + (static_cast<size_t>(b) * a.N + node) * a.words;
-    auto word = [&](int w) { return w < 0 ? ~0ull : w >= a.words ? 0ull : a.words == 1 ? only : row[w]; };
-    const int w = first >> 6, shift = first & 63;
-    bits = static_cast<u32>(word(w) >> shift);
-    if (shift > 56) bits |= static_cast<u32>(word(w + 1) << (64 - shift));
-  } else {
-    const int k = node + 1 - first;
-    bits = k >= 8 ? 0xFFu : k <= 0 ? 0u : (1u << k) - 1;
+// ---------------------------------------------------------------- 32 rows per wave
+// Both products on v_mfma_f32_32x32x16_bf16, which holds the vector port for 12 of its 32 clocks, that of 16 rows for 10 of 16.  Lane (r = l % 32, h = l / 32):
+//   scores    first operand: key r of the tile, half of its channels.  The lane ends up with the scores of keys 8a + 4h + i, i < 4, for its query --
+//   values    -- which are eight keys each of the second product's two steps: keys 16t + 4h .. + 3 and 8 more on.  Its first operand: the same keys of D/32 channels.
+// The waves of a work-group go through the tiles together, each converts the values of 16 keys of the next step for all of them, and waits for the others once per
+// step (64 keys for four waves, 128 for eight, of which one work-group fills a compute unit; two of four end 20% apart, as one is served first throughout).  With the
+// scores a tile ahead, the second product a tile behind and the exponentials between them there is always something to issue.
+// 4 trees of 208 rows over 60 000 - 131 000 tokens: 440 us (0.78 PFLOP/s, 0.84 with the rows that fill up the last wave's 32; a large library product reaches
+// 1.2), by work-groups of four waves 510.  16 trees of 240 rows over 1 024 - 8 191: 110 us, by four 118.  The matrix cores are busy for half of the clocks; finer
+// interleaving, priorities and a deeper ring changed nothing, and the clock falls to 1.7 - 2.0 GHz meanwhile: it is the power that bounds it.
+template <int D> struct Keys32 {
+  u32 k[D / 64][4], ks[D / 64];  // 32 channels each, 64 s + 32 h
+  Keys32() = default;
+  __device__ __forceinline__ explicit Keys32(const uint8_t* tile) {
+    using X = Tile<D>;
+    const u32 lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
+#pragma unroll
+    for (int s = 0; s < D / 64; ++s) {
+      const u32x4 w = *reinterpret_cast<const u32x4*>(tile + X::key_slot(r, 2 * s + h) * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) k[s][j] = w[j];
+      ks[s] = tile[2 * X::kCodes + r * (D / 32) + 2 * s + h];
+    }
   }
-  const int k = n - first;
-  return bits & (k >= 8 ? 0xFFu : k <= 0 ? 0u : (1u << k) - 1);
+};
+template <int D> struct Values32 {
+  static constexpr int C = D / 32;  // channels of a lane: C r ..
+  u32 v[2][4], vs[2];               // of octet 2t + o: tokens 4h .. 4h + 3, a dword column's codes, their scales
+  __device__ __forceinline__ Values32(const uint8_t* tile, u32 t) {
+    using X = Tile<D>;
+    const u32 lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
+#pragma unroll
+    for (u32 o = 0; o < 2; ++o) {
+      const u32x4 w = *reinterpret_cast<const u32x4*>(tile + X::kCodes + X::value_slot(2 * t + o, r * C / 8, h) * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[o][j] = w[j];
+      vs[o] = *reinterpret_cast<const u32*>(tile + 2 * X::kCodes + (D <= 128 ? 128 : 256) + (2 * t + o) * (D / 4) + r * C / 32 * 8 + 4 * h);
+    }
+  }
+  // Only the first `there` of the step's 16 tokens count, and none of its octets in `bad`: elsewhere memory holds anything, and 0 times that has to be 0.
+  __device__ __forceinline__ void cut(int there, u32 bad) {
+    const int h = threadIdx.x % kWave / 32;
+#pragma unroll
+    for (int o = 0; o < 2; ++o) {
+      const int n = bad >> o & 1 ? 0 : there - 8 * o - 4 * h;
+      vs[o] = n >= 4 ? vs[o] : n <= 0 ? 0 : vs[o] & ((1u << (8 * n)) - 1);
+    }
+  }
+  // f(block, fragment) for blocks 2 BYTE and 2 BYTE + 1 of the C: channel C r + block.
+  template <int BYTE, typename F> __device__ __forceinline__ void pair(F f) const {
+    const u32 shift = D == 64 ? (threadIdx.x & 3) * 8 : D == 128 ? (threadIdx.x & 1) * 16 : 0;
+    u32 w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = v[j / 4][j % 4] >> shift;
+    const u32 s[8] = {scale_at<0>(vs[0]), scale_at<1>(vs[0]), scale_at<2>(vs[0]), scale_at<3>(vs[0]),
+                      scale_at<0>(vs[1]), scale_at<1>(vs[1]), scale_at<2>(vs[1]), scale_at<3>(vs[1])};
+    u32 y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = decode<BYTE>(w[j], s[j]);
+    f(2 * BYTE, as_bf16x8(low_halves(y[0], y[1]), low_halves(y[2], y[3]), low_halves(y[4], y[5]), low_halves(y[6], y[7])));
+    f(2 * BYTE + 1, as_bf16x8(high_halves(y[0], y[1]), high_halves(y[2], y[3]), high_halves(y[4], y[5]), high_halves(y[6], y[7])));
+  }
+};
+
+template <int D, typename T> struct Queries32 {
+  static constexpr int S = D / 16, TERMS = std::is_same<T, float>::value ? 3 : 1;  // steps of 16 channels
+  bf16x8 q[TERMS][S];
+  __device__ __forceinline__ void load(const T* row, bool live) {
+    const int h = threadIdx.x % kWave / 32;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      u32 t[4][TERMS];
+      const Eight e = load_eight(row + s / 4 * 64 + h * 32 + s % 4 * 8);
+#pragma unroll
+      for (int p = 0; p < 4; ++p) split_pair<TERMS>(live ? e.x[2 * p] : 0.0f, live ? e.x[2 * p + 1] : 0.0f, t[p]);
+#pragma unroll
+      for (int k = 0; k < TERMS; ++k) q[k][s] = as_bf16x8(t[0][k], t[1][k], t[2][k], t[3][k]);
+    }
+  }
+  static constexpr int kSteps = S * TERMS;
+  __device__ __forceinline__ void step(int i, f32x16& sc, const Keys32<D>& x) const {
+    const int s = i / TERMS, t = TERMS - 1 - i % TERMS;
+    const u32 scale = scale_at<0>(x.ks[s / 4]), w = x.k[s / 4][s % 4];
+    const bf16x8 k = as_bf16x8(decode<0>(w, scale), decode<1>(w, scale), decode<2>(w, scale), decode<3>(w, scale));
+    sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[t][s], i == 0 ? f32x16{} : sc, 0, 0, 0);
+  }
+};
+
+// Where a quarter of a lane's results goes: [block][i] is channel C (8 quarter + 4 h + i) + block of its row.
+template <int D, typename T>
+__device__ __forceinline__ void write_wide(const AttnArgs& a, int b, int head, int node0, int row0, int rows, int quarter, const f32x4 (&o)[D / 32], float m, float l) {
+  constexpr int C = D / 32;
+  const int lane = threadIdx.x % kWave, h = lane / 32, row = row0 + lane % 32;
+  if (row >= rows) return;
+  const int in = row / a.group, node = node0 + in, q_head = head * a.group + row - in * a.group;
+  const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
+  T* at = static_cast<T*>(a.out) + b * a.out_request + node * a.out_node + q_head * a.out_head + C * (8 * quarter + 4 * h);
+  float x[4 * C];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int k = 0; k < C; ++k) x[i * C + k] = o[k][i] * inverse;
+#pragma unroll
+  for (int i = 0; i < 4 * C; i += 8) {
+    if constexpr (std::is_same<T, float>::value) {
+      *reinterpret_cast<f32x4*>(at + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+      *reinterpret_cast<f32x4*>(at + i + 4) = f32x4{x[i + 4], x[i + 5], x[i + 6], x[i + 7]};
+    } else {
+      *reinterpret_cast<u32x4*>(at + i) = u32x4{round_pair(x[i], x[i + 1]), round_pair(x[i + 2], x[i + 3]), round_pair(x[i + 4], x[i + 5]), round_pair(x[i + 6], x[i + 7])};
+    }
+  }
+  if (a.lse && h == 0 && quarter == 0) a.lse[(static_cast<size_t>(b) * a.N + node) * a.q_heads + q_head] = log_sum(m, l);
 }
 
-// Probabilities of a tile's keys as the second product's second operand: TERMS bf16 terms each.
-template <int D, int RB, typename T> struct Weights { u32 p[Wave<D, RB, T>::TERMS][RB][4]; };
+template <int D_, typename T_, int WAVES> struct Wide {
+  using T = T_;
+  static constexpr int D = D_, MODE = ROWS, kRows = 32, kGroupWaves = WAVES;
+  static constexpr int C = D / 32;              // blocks of 32 channels of the result
+  static constexpr int kParts = 4 * C;          // four numbers of a lane each
+  static constexpr int TERMS = std::is_same<T, float>::value ? 3 : 1;
+  static constexpr bool kAhead = TERMS == 1;    // scores a tile ahead, the second product a tile behind (three terms' operands leave no registers for it)
+  static constexpr int kNext = kAhead ? 2 : 1;  // how far in front of a tile keys are loaded
+  using Q = Queries32<D, T>;
+  Q q;
+  f32x16 sc[kAhead ? 2 : 1];                    // scores of this tile and the next
+  Keys32<D> next;                               // of the next tile
+  u32 p[TERMS][2][4];                           // of the tile before: probabilities, in terms, two steps of the product with
+  u32x4 v[2 * C];                               // its values
+  f32x16 o[C];                                  // [block][i]: channel C (8 (i/4) + 4h + i%4) + block
+  float m, l;
+  int node;                                     // of this lane's row; < 0: no row
+  unsigned long long word;
 
-// One tile.  `plain` (the same for the wave): every row sees all of it, and all of it is there.  Otherwise: request b has n nodes behind
-// `len` tokens, the tile begins at t0; `poison`: the lane's octet has no page.
-template <int D, int RB, typename T>
-__device__ __forceinline__ void weigh(const AttnArgs& a, Wave<D, RB, T>& w, f32x4 (&sc)[2][RB], bool plain, int b, int len, int n, int t0, bool poison,
-                                      Weights<D, RB, T>& y) {
-  constexpr int NF = D / 16, TERMS = Wave<D, RB, T>::TERMS;
-  const float c = a.scale_log2;
-  __builtin_amdgcn_sched_barrier(0);  // (the values' conversions would be brought up to here, and their results kept)
-  if (!plain) {
-    const int first = t0 + static_cast<int>(threadIdx.x % kWave / 16) * 8 - len;
+  __device__ __forceinline__ void start(const AttnArgs& a, int b, int head, int node0, int row0, int rows) {
+    const RowOf<T> row(a, b, head, node0, row0 + threadIdx.x % 32, rows);
+    node = row.node;
+    word = row.word;
+    q.load(row.q, node >= 0);
+    m = kFloor;
+    l = 0.0f;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const u32 sees = w.node[rb] < 0 ? 0u : seen(a, w.word[rb], b, w.node[rb], n, first);
+    for (int k = 0; k < C; ++k) {
+      o[k] = f32x16{};
+      v[k] = v[C + k] = u32x4{0, 0, 0, 0};
+    }
+    clear_before();
+  }
+  // A step's values as operands, to `values` [tile][2 C][64]: 16 keys' by each wave.  `tiles`: the step's, keys t0 ..
+  __device__ __forceinline__ static Values32<D> sixteen(const uint8_t* tiles, const u32* sh_bad, int t0, int end) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const u32 bad = __builtin_amdgcn_readfirstlane(sh_bad[wave / 2]) >> (wave % 2 * 2);
+    t0 += wave * 16;
+    Values32<D> x(tiles + wave / 2 * Tile<D>::kBytes, wave % 2);
+    if (t0 + 16 > end || (bad & 3)) x.cut(end - t0, bad);
+    return x;
+  }
+  template <int I> __device__ __forceinline__ static void convert(const Values32<D>& x, u32x4* values) {  // part I of C / 2
+    u32x4* const at = values + threadIdx.x / kWave * C * kWave + threadIdx.x % kWave;
+    if constexpr (I < C / 2) x.template pair<I>([&](int k, bf16x8 v) { at[k * kWave] = __builtin_bit_cast(u32x4, v); });
+  }
+  __device__ __forceinline__ void first_product(f32x16& to) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+    for (int i = 0; i < Q::kSteps; ++i) q.step(i, to, next);
+  }
+  __device__ __forceinline__ void begin(const uint8_t* tiles) {
+    next = Keys32<D>(tiles);
+    if (!kAhead) return;
+    first_product(sc[0]);
+    next = Keys32<D>(tiles + Tile<D>::kBytes);
+  }
+  __device__ __forceinline__ void clear_before() {
+#pragma unroll
+    for (int i = 0; i < TERMS * 8; ++i) p[i / 8][i % 8 / 4][i % 4] = 0;
+  }
+  // The second product of the tile before, in kAdds steps.
+  static constexpr int kAdds = 2 * C * TERMS;
+  __device__ __forceinline__ void add(int i) {
+    const int t = i / (C * TERMS), k = i % (C * TERMS) / TERMS, x = TERMS - 1 - i % TERMS;
+    o[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[t * C + k]), as_bf16x8(p[x][t][0], p[x][t][1], p[x][t][2], p[x][t][3]), o[k], 0, 0, 0);
+  }
+  __device__ __forceinline__ void add_values() {
+#pragma unroll
+    for (int i = 0; i < kAdds; ++i) add(i);
+  }
+  // A tile (as Narrow::tile says), an even or an odd one, its values as operands at `values`; in the meantime f(0), f(1) ...  kAhead: on the matrix cores are the next
+  // tile's scores and the product with the values of the tile before.  `after`: the tile whose keys are loaded meanwhile.
+  template <int I, typename F>
+  __device__ __forceinline__ void tile(const AttnArgs& a, const uint8_t* after, const u32x4* values, u32 bad, int b, int len, int n, int t0, F f) {
+    const float c = a.scale_log2;
+    f32x16& s = sc[kAhead ? I : 0];
+    if constexpr (!kAhead) first_product(s);
+    if (t0 + kTile > len || bad) {
+      const int h = threadIdx.x % kWave / 32;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const u32 sees = node < 0 ? 0u : seen(a, word, b, node, n, t0 + 8 * k - len) >> (4 * h);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float s = poison ? __builtin_nanf("") : sc[k][rb][i];
-          sc[k][rb][i] = sees >> (4 * k + i) & 1 ? s : -__builtin_inff();
+          const float x = bad >> k & 1 ? __builtin_nanf("") : s[4 * k + i];
+          s[4 * k + i] = sees >> i & 1 ? x : -__builtin_inff();
         }
+      }
     }
-  }
-  float top[RB];
-  bool up = false;
+    float top = max3(s[0], s[1], s[2]);
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    float t = max3(sc[0][rb][0], sc[0][rb][1], sc[0][rb][2]);
-    t = max3(t, sc[0][rb][3], sc[1][rb][0]);
-    t = max3(t, sc[1][rb][1], sc[1][rb][2]);
-    t = max3(t, sc[1][rb][3], t);
-    top[rb] = t * c;
-    up |= top[rb] > w.m[rb] + kSlack;
-  }
-  if (__any(up)) {  // seldom after the first tiles
+    for (int i = 3; i < 15; i += 2) top = max3(top, s[i], s[i + 1]);
+    top = max3(top, s[15], top) * c;
+    if (__any(top > m + kSlack)) {  // seldom after the first tiles
+      if (kAhead) {
+        add_values();
+        clear_before();
+      }
+      top = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
+      const float shrink = __builtin_amdgcn_exp2f(m - top);
+      m = top;
+      l *= shrink;
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const float m = fmaxf(w.m[rb], over_groups_max(top[rb]));
-      const float shrink = __builtin_amdgcn_exp2f(w.m[rb] - m);
-      w.m[rb] = m;
-      w.l[rb] *= shrink;
-#pragma unroll
-      for (int f = 0; f < NF; ++f) w.o[f][rb] *= shrink;
+      for (int k = 0; k < C; ++k) o[k] *= shrink;
     }
-  }
+    __builtin_amdgcn_sched_barrier(0);
+    auto weigh = [&](int j, u32 (&to)[TERMS][2][4]) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * j], c, -m)), e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], c, -m));
+      l += e0 + e1;
+      u32 x[TERMS];
+      split_pair<TERMS>(e0, e1, x);
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
+      for (int k = 0; k < TERMS; ++k) to[k][j / 4][j % 4] = x[k];
+    };
+    auto load = [&](int k) { v[k] = values[k * kWave + threadIdx.x % kWave]; };
+    if constexpr (kAhead) {
+      // Between two matrix instructions what the vector port can do while the first runs.
+      constexpr int kAll = Q::kSteps + kAdds;
+      u32 e[TERMS][2][4];
+      each<Q::kSteps>([&](auto i) {
+        q.step(i, sc[1 - I], next);
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[h / 2][rb][h % 2 * 2], c, -w.m[rb]));
-      const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[h / 2][rb][h % 2 * 2 + 1], c, -w.m[rb]));
-      w.l[rb] += e0 + e1;
-      u32 t[TERMS];
-      split_pair<TERMS>(e0, e1, t);
+        for (int j = i * 8 / kAll; j < (i + 1) * 8 / kAll; ++j) weigh(j, e);
+        f(i);
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      next = Keys32<D>(after);
+      each<kAdds>([&](auto i) {
+        add(i);
 #pragma unroll
-      for (int k = 0; k < TERMS; ++k) y.p[k][rb][h] = t[k];
-    }
-  }
-  __builtin_amdgcn_sched_barrier(0);
-}
-template <int D, int RB, typename T>
-__device__ __forceinline__ void add_values(Wave<D, RB, T>& w, const Weights<D, RB, T>& y, int n, bf16x8 values) {
+        for (int j = (Q::kSteps + i) * 8 / kAll; j < (Q::kSteps + i + 1) * 8 / kAll; ++j) weigh(j, e);
+        load(i);
+        __builtin_amdgcn_sched_barrier(0);
+      });
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-    for (int t = Wave<D, RB, T>::TERMS - 1; t >= 0; --t)
-      w.o[n][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(values, as_bf16x8(y.p[t][rb][0], y.p[t][rb][1], y.p[t][rb][2], y.p[t][rb][3]), w.o[n][rb], 0, 0, 0);
-}
-
-// Where the results of a lane go: element [f][i] of its row among the 16 from `row0` on is channel (4g + i) * D/16 + f0 + f.
-template <int D, int F, typename T>
-__device__ __forceinline__ void write_part(const AttnArgs& a, int b, int head, int node0, int row0, int rows, int f0, const f32x4 (&o)[F], float m, float l) {
-  constexpr int C = D / 16;
-  const int lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
-  const int row = row0 + r;
-  if (row >= rows) return;
-  const int in = row / a.group, node = node0 + in, h = head * a.group + row - in * a.group;
-  const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
-  T* at = static_cast<T*>(a.out) + b * a.out_request + node * a.out_node + h * a.out_head + g * (4 * C) + f0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float x[F];
-#pragma unroll
-    for (int f = 0; f < F; ++f) x[f] = o[f][i] * inverse;
-    if constexpr (std::is_same<T, float>::value) {
-      if constexpr (F == 1) at[i * C] = x[0];
-      else if constexpr (F == 2) *reinterpret_cast<f32x2*>(at + i * C) = f32x2{x[0], x[1]};
-      else
-#pragma unroll
-        for (int f = 0; f < F; f += 4) *reinterpret_cast<f32x4*>(at + i * C + f) = f32x4{x[f], x[f + 1], x[f + 2], x[f + 3]};
+      for (int i = 0; i < 8; ++i) p[0][i / 4][i % 4] = e[0][i / 4][i % 4];
     } else {
-      if constexpr (F == 1) at[i * C] = static_cast<bf16_t>(round_pair(x[0], 0.0f));
-      else if constexpr (F == 2) *reinterpret_cast<u32*>(at + i * C) = round_pair(x[0], x[1]);
-      else if constexpr (F == 4) *reinterpret_cast<u32x2*>(at + i * C) = u32x2{round_pair(x[0], x[1]), round_pair(x[2], x[3])};
-      else
+      load(0);
+      load(1);
+      next = Keys32<D>(after);
 #pragma unroll
-        for (int f = 0; f < F; f += 8)
-          *reinterpret_cast<u32x4*>(at + i * C + f) = u32x4{round_pair(x[f], x[f + 1]), round_pair(x[f + 2], x[f + 3]),
-                                                            round_pair(x[f + 4], x[f + 5]), round_pair(x[f + 6], x[f + 7])};
+      for (int j = 0; j < 8; ++j) weigh(j, p);
+      each<C / 2>(f);
+      each<kAdds>([&](auto i) {
+        add(i);
+        if constexpr (i % TERMS == TERMS - 1 && i / TERMS + 2 < 2 * C) load(i / TERMS + 2);
+        __builtin_amdgcn_sched_barrier(0);
+      });
     }
   }
-  if (a.lse && g == 0 && f0 == 0)
-    a.lse[(static_cast<size_t>(b) * a.N + node) * a.q_heads + h] =
-        l == 0.0f ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
-}
+  __device__ __forceinline__ void finish() {
+    if (kAhead) add_values();
+    l += __shfl_xor(l, 32);
+  }
+  __device__ __forceinline__ f32x4 part(int i) const { return f32x4{o[i / 4][i % 4 * 4], o[i / 4][i % 4 * 4 + 1], o[i / 4][i % 4 * 4 + 2], o[i / 4][i % 4 * 4 + 3]}; }
+  __device__ __forceinline__ void write(const AttnArgs& a, int b, int head, int node0, int row0, int rows) const {
+#pragma unroll
+    for (int quarter = 0; quarter < 4; ++quarter) {
+      f32x4 x[C];
+#pragma unroll
+      for (int k = 0; k < C; ++k) x[k] = part(4 * k + quarter);
+      write_wide<D, T>(a, b, head, node0, row0, rows, quarter, x, m, l);
+    }
+  }
+  template <typename P> __device__ __forceinline__ void save(const P& piece) const {
+    const int lane = threadIdx.x % kWave;
+    if (lane < 32) {
+      piece.reference(lane) = m;
+      piece.sum(lane) = l;
+    }
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) piece.part(i, lane) = part(i);
+  }
+  static constexpr int kStrips = WAVES, kStripRows = 32, kQuarter = C;
+  __device__ static __forceinline__ int strip_row(int) { return threadIdx.x % 32; }
+  __device__ static __forceinline__ int strip_wave(int strip) { return strip; }
+  __device__ static __forceinline__ int strip_part(int, int quarter, int i) { return 4 * i + quarter; }
+  __device__ static __forceinline__ void write_quarter(const AttnArgs& a, int b, int head, int node0, int strip, int rows, int quarter, const f32x4 (&x)[C], float m,
+                                                       float l) {
+    write_wide<D, T>(a, b, head, node0, strip * 32, rows, quarter, x, m, l);
+  }
+};
 
-// A piece in the workspace: [16 RB] references, [16 RB] sums, then the results lane by lane, [RB][D/16][64] of four.
-template <int D, int RB> struct Piece {
-  static constexpr int kFloats = 32 * RB + RB * (D / 16) * 256;
+// ---------------------------------------------------------------- kernels
+// A wave's piece in the workspace: its rows' references, their sums, then the results lane by lane.
+template <typename W> struct Piece {
+  static constexpr int kFloats = 2 * W::kRows + W::kParts * 256;
   float* at;
   __device__ __forceinline__ Piece(float* partial, long slot) : at(partial + slot * kFloats) {}
   __device__ __forceinline__ float& reference(int row) const { return at[row]; }
-  __device__ __forceinline__ float& sum(int row) const { return at[16 * RB + row]; }
-  __device__ __forceinline__ f32x4& part(int rb, int f, int lane) const {
-    return reinterpret_cast<f32x4*>(at + 32 * RB)[(rb * (D / 16) + f) * kWave + lane];
-  }
+  __device__ __forceinline__ float& sum(int row) const { return at[W::kRows + row]; }
+  __device__ __forceinline__ f32x4& part(int i, int lane) const { return reinterpret_cast<f32x4*>(at + 2 * W::kRows)[i * kWave + lane]; }
 };
 
 // Rows that see nothing because their request has fewer nodes (or no sequence): zeros.
 template <typename T, int D> __device__ __forceinline__ void clear_rows(const AttnArgs& a, int b, int n) {
   const long items = static_cast<long>(a.N - n) * a.q_heads * (D / 8);
-  for (long i = threadIdx.x; i < items; i += kThreads) {
+  for (long i = threadIdx.x; i < items; i += blockDim.x) {
     const int c = static_cast<int>(i % (D / 8)), h = static_cast<int>(i / (D / 8) % a.q_heads), node = n + static_cast<int>(i / (D / 8) / a.q_heads);
     T* at = static_cast<T*>(a.out) + b * a.out_request + node * a.out_node + h * a.out_head + c * 8;
     const u32 none[4] = {0, 0, 0, 0};
@@ -717,34 +742,37 @@ template <typename T, int D> __device__ __forceinline__ void clear_rows(const At
   }
 }
 
-enum { KEYS = 0, ROWS = 1 };  // what the waves of a work-group divide between them
-template <int MODE, int RB> constexpr int rows_per_block = MODE == KEYS ? 16 * RB : 64 * RB;
 // Work-groups that have to fit a compute unit beside each other: what the compiler may give a wave of registers, and the ring of LDS.
-constexpr int per_unit(int D, int RB, bool f32) { return D == 256 ? (RB == 1 && !f32 ? 2 : 1) : f32 ? 2 : RB == 1 ? 3 : 2; }
-template <int D, int RB, typename T> constexpr int kPerUnit = per_unit(D, RB, std::is_same<T, float>::value);
-constexpr int values_bytes(int D, int mode) { return mode == ROWS ? kWaves * (D / 16) * 1024 : 0; }  // of a unit's values as operands
-constexpr int stages_of(int D, int mode, int groups) {  // units in the ring, the one that is worked on among them
-  const int n = (160 * 1024 / groups - 1024 - values_bytes(D, mode)) / (kWaves * (32 * D + (D <= 128 ? 256 : 512)));
+constexpr int per_unit(int D, int mode, int waves, int rows, bool f32) {
+  if (mode == KEYS) return (D == 256 ? 1 : 2) + (rows == 16 && !f32 ? 1 : 0);
+  return D == 256 || waves > kWaves ? 1 : 2;
+}
+template <typename W> constexpr int kPerUnit = per_unit(W::D, W::MODE, W::kGroupWaves, W::kRows, std::is_same<typename W::T, float>::value);
+template <typename W> constexpr int kValuesBytes = W::MODE == ROWS ? W::kGroupWaves * W::D * 64 : 16;  // of two steps' values as operands
+template <typename W> constexpr int stages_of() {  // units in the ring, those that are worked on among them
+  constexpr int n = (160 * 1024 / kPerUnit<W> - 1024 - kValuesBytes<W>) / (kWaves * Tile<W::D>::kBytes);
   return n > 4 ? 4 : n;
 }
 
-template <int D, int RB, typename T, int MODE, bool UNIFORM>
-__global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kernel(AttnArgs a) {
+template <typename W, bool UNIFORM>
+__global__ void __launch_bounds__(W::kGroupWaves * kWave, kPerUnit<W> * W::kGroupWaves / kWaves) attention_kernel(AttnArgs a) {
+  constexpr int D = W::D, MODE = W::MODE, GROUP = W::kGroupWaves, STAGES = stages_of<W>();
+  // Units in flight behind the one that is waited for (in mode ROWS a step is half a unit, or a whole one by eight waves):
+  constexpr int AHEAD = GROUP > kWaves ? STAGES - 3 : STAGES - 2;
   using X = Tile<D>;
-  constexpr int NF = D / 16, STAGES = stages_of(D, MODE, kPerUnit<D, RB, T>);
-  static_assert(STAGES >= 2, "a unit in flight while another is worked on");
-  constexpr int kJoin = MODE == KEYS ? 2 * RB * NF * 1024 : 0;  // bytes for two waves' results
+  static_assert(AHEAD >= 0, "a unit in flight while another is worked on");
+  constexpr int kJoin = MODE == KEYS ? 2 * W::kParts * 1024 : 0;  // bytes for two waves' results
   constexpr int kRing = STAGES * kWaves * X::kBytes;
   __shared__ __attribute__((aligned(1024))) uint8_t sh_ring[kRing > kJoin ? kRing : kJoin];
-  __shared__ __attribute__((aligned(16))) u32x4 sh_values[MODE == ROWS ? kWaves : 1][MODE == ROWS ? NF : 1][kWave];
+  __shared__ __attribute__((aligned(16))) u32x4 sh_values[kValuesBytes<W> / 16];
   __shared__ u32 sh_bad[STAGES][kWaves];
-  __shared__ float sh_m[MODE == KEYS ? 4 : 1][16 * RB], sh_l[MODE == KEYS ? 4 : 1][16 * RB];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
+  __shared__ float sh_m[MODE == KEYS ? kWaves * W::kRows : 1], sh_l[MODE == KEYS ? kWaves * W::kRows : 1];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
 
   if (a.n_new || a.seqs)  // (otherwise every request has N nodes)
     for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
       const int n = Request(a, b).n;
-      if (n < a.N) clear_rows<T, D>(a, b, n);
+      if (n < a.N) clear_rows<typename W::T, D>(a, b, n);
     }
   Deal deal(a, gridDim.x);
   const u32 share = deal.share;
@@ -756,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kern
   const u32 unit0 = static_cast<u32>(my_begin), unit1 = static_cast<u32>(min(my_begin + share, static_cast<unsigned long long>(deal.total)));
   const u32 ring = lds_address(sh_ring);
 
-  Wave<D, RB, T> w;
+  W w;
   for (u32 u = unit0; u < unit1;) {
     const auto p = deal.find(u);
     if (p.count == 0) {
@@ -766,155 +794,109 @@ __global__ void __launch_bounds__(kThreads, (kPerUnit<D, RB, T>)) attention_kern
     const u32 taken = min(p.count - p.offset, unit1 - u);
     const bool whole = taken == p.count;
     const int units = static_cast<int>(deal.whole ? p.r.block_units(a, p.block) : taken);
-    const int node0 = p.block * a.nodes, rows = min(a.nodes, p.r.n - node0) * a.group, row0 = MODE == ROWS ? wave * 16 * RB : 0;
+    const int node0 = p.block * a.nodes, rows = min(a.nodes, p.r.n - node0) * a.group, row0 = MODE == ROWS ? wave * W::kRows : 0;
     const int len = p.r.len, n = p.r.n, end = len + n;
-    // no row of this wave sees keys from here on (-1: it has no rows)
-    const int limit = row0 >= rows ? 0 : a.mask ? end : len + 1 + node0 + (min(rows, row0 + 16 * RB) - 1) / a.group;
+    // no row of this wave sees keys from here on (0: it has no rows)
+    const int limit = row0 >= rows ? 0 : a.mask ? end : len + 1 + node0 + (min(rows, row0 + W::kRows) - 1) / a.group;
     const int from = static_cast<int>(p.offset) * kUnit;
     // (in front of the queries' loads; LDS is free: the piece before ended with a barrier)
-    Fetch<D, UNIFORM> fetch(a, sequence_of(a.c, a.seqs, p.b), p.head, end, from + wave * kTile);
+    Fetch<D, UNIFORM> fetch(a, sequence_of(a.c, a.seqs, p.b), p.head, end, from + wave % kWaves * kTile);
     u32 stage = 0;
     auto issue = [&](u32 to) {
       const u32 bad = fetch.next(ring + (to * kWaves + wave) * X::kBytes);
       if (lane == 0) sh_bad[to][wave] = bad;
     };
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i)
-      if (i < units) issue(i);
+    for (int i = 0; i <= AHEAD; ++i)
+      if (i < units && wave < kWaves) issue(i);
     w.start(a, p.b, p.head, node0, row0, rows);
 
-    for (int unit = 0; unit < units; ++unit) {
-      // this wave's tile of the unit is there; with a barrier, all are, and nobody reads the unit before any more
-      if (unit + STAGES - 1 <= units) arrived<(STAGES - 2) * X::kLoads>();
+    // This wave's tile of a unit, in place `at` of the ring, is there; with a barrier (which leaves alone what is in flight from memory) those of others, and everybody
+    // is done with the step before.
+    auto wait_for = [&](int unit) {
+      if (unit + AHEAD < units) arrived<AHEAD * X::kLoads>();
       else arrived<0>();
-      if (MODE == ROWS) __builtin_amdgcn_s_barrier();
-      if (unit + STAGES - 1 < units) issue(stage == 0 ? STAGES - 1 : stage - 1);
-      const int t_unit = from + unit * kUnit;
-      if constexpr (MODE == KEYS) {
-        const int t0 = t_unit + wave * kTile;
+    };
+    auto issue_behind = [&](int unit, u32 at) {
+      if (unit + AHEAD + 1 < units) issue(at + AHEAD + 1 >= STAGES ? at + AHEAD + 1 - STAGES : at + AHEAD + 1);
+    };
+    if constexpr (MODE == KEYS) {
+      for (int unit = 0; unit < units; ++unit) {
+        wait_for(unit);
+        issue_behind(unit, stage);
+        const int t0 = from + unit * kUnit + wave * kTile;
         if (t0 < limit) {
-          const uint8_t* tile = sh_ring + (stage * kWaves + wave) * X::kBytes;
           const u32 bad = __builtin_amdgcn_readfirstlane(sh_bad[stage][wave]);
-          const bool plain = t0 + kTile <= len && bad == 0, poison = bad >> g & 1;
-          const Keys<D> keys(tile);
-          Values<D> values(tile);
-          f32x4 sc[2][RB];
-          w.q.scores(keys, sc);
-          Weights<D, RB, T> y;
-          weigh<D, RB, T>(a, w, sc, plain, p.b, len, n, t0, poison, y);
-          if (!plain) values.cut(poison ? 0 : end - t0 - 8 * g);
-          values.each([&](int f, bf16x8 v) { add_values<D, RB, T>(w, y, f, v); });
+          w.tile(a, sh_ring + (stage * kWaves + wave) * X::kBytes, t0 + kTile <= len && bad == 0, p.b, len, n, t0, bad);
         }
-      } else {
-        // A tile's scores are under way on the matrix cores while the one before it is weighed, the first one's while each wave
-        // converts the values of its tile for all.
-        const uint8_t* const tiles = sh_ring + stage * kWaves * X::kBytes;
-        f32x4 sc[2][2][RB];
-        w.q.scores(Keys<D>(tiles), sc[0]);
-        {
-          const int t0 = t_unit + wave * kTile;
-          const u32 bad = __builtin_amdgcn_readfirstlane(sh_bad[stage][wave]);
-          Values<D> values(sh_ring + (stage * kWaves + wave) * X::kBytes);
-          if (t0 + kTile > end || bad) values.cut(bad >> g & 1 ? 0 : end - t0 - 8 * g);
-          values.each([&](int f, bf16x8 v) { sh_values[wave][f][lane] = __builtin_bit_cast(u32x4, v); });
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (what is in flight from memory stays so)
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) {
-          const int t0 = t_unit + i * kTile;
-          if (t0 >= limit) break;
-          const u32 bad = __builtin_amdgcn_readfirstlane(sh_bad[stage][i]);
-          u32x4 v[NF];
-#pragma unroll
-          for (int f = 0; f < NF; ++f) v[f] = sh_values[i][f][lane];
-          if (i + 1 < kWaves) w.q.scores(Keys<D>(tiles + (i + 1) * X::kBytes), sc[(i + 1) % 2]);
-          Weights<D, RB, T> y;
-          weigh<D, RB, T>(a, w, sc[i % 2], t0 + kTile <= len && bad == 0, p.b, len, n, t0, bad >> g & 1, y);
-#pragma unroll
-          for (int f = 0; f < NF; ++f) add_values<D, RB, T>(w, y, f, __builtin_bit_cast(bf16x8, v[f]));
-        }
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
       }
-      stage = stage + 1 == STAGES ? 0 : stage + 1;
+    } else {
+      // While a step is worked on, the values of the next one are converted.  Its tiles are those that two of four waves have fetched, or four of eight; the
+      // places of the step before are the same waves', to be filled again.
+      constexpr int TILES = GROUP / 2;
+      u32x4 *here = sh_values, *there = sh_values + kValuesBytes<W> / 32;
+      int t0 = from;
+      auto next_step = [&](int unit, u32 at, int first) {
+        const bool mine = wave >= first && wave < first + TILES;
+        if (mine) wait_for(unit);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (mine) issue_behind(unit, at);
+      };
+      auto step = [&](const uint8_t* now, const u32* bad, const uint8_t* then, const u32* bad_then) {
+        const auto x = W::sixteen(then, bad_then, t0 + TILES * kTile, end);
+        each<TILES>([&](auto number) {
+          constexpr int I = decltype(number)::value;
+          auto convert = [&](auto part) {
+            if constexpr (I == 0) W::template convert<decltype(part)::value>(x, there);
+          };
+          if (t0 < limit)
+            w.template tile<I % 2>(a, I + W::kNext < TILES ? now + (I + W::kNext) * X::kBytes : then + (I + W::kNext - TILES) * X::kBytes, here + I * (D / 16) * kWave,
+                                   __builtin_amdgcn_readfirstlane(bad[I]), p.b, len, n, t0, convert);
+          else each<D / 64>(convert);
+          t0 += kTile;
+        });
+        u32x4* const done = here;
+        here = there;
+        there = done;
+      };
+      next_step(0, 0, 0);
+      each<D / 64>([&, x = W::sixteen(sh_ring, sh_bad[0], t0, end)](auto part) { W::template convert<decltype(part)::value>(x, here); });
+      w.begin(sh_ring);
+      for (int unit = 0; unit < units; ++unit) {
+        const uint8_t* const now = sh_ring + stage * kWaves * X::kBytes;
+        const u32* const bad = sh_bad[stage];
+        const u32 following = stage + 1 == STAGES ? 0 : stage + 1;
+        const uint8_t* const then = sh_ring + following * kWaves * X::kBytes;
+        if constexpr (GROUP > kWaves) {
+          next_step(unit + 1, following, 0);
+          step(now, bad, then, sh_bad[following]);
+        } else {
+          next_step(unit, stage, 2);
+          step(now, bad, now + 2 * X::kBytes, bad + 2);
+          next_step(unit + 1, following, 0);
+          step(now + 2 * X::kBytes, bad + 2, then, sh_bad[following]);
+        }
+        stage = following;
+      }
     }
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) w.l[rb] = over_groups_sum(w.l[rb]);
+    w.finish();
     __syncthreads();  // the ring is free
-
-    if (MODE == KEYS) {
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-        if (lane < 16) {
-          sh_m[wave][rb * 16 + r] = w.m[rb];
-          sh_l[wave][rb * 16 + r] = w.l[rb];
-        }
-      __syncthreads();
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        float m = kFloor, l = 0.0f;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) m = fmaxf(m, sh_m[v][rb * 16 + r]);
-#pragma unroll
-        for (int v = 0; v < 4; ++v) l += sh_l[v][rb * 16 + r] * __builtin_amdgcn_exp2f(sh_m[v][rb * 16 + r] - m);
-        const float shrink = __builtin_amdgcn_exp2f(w.m[rb] - m);
-#pragma unroll
-        for (int f = 0; f < NF; ++f) w.o[f][rb] *= shrink;
-        w.m[rb] = m;
-        w.l[rb] = l;
-      }
-      // waves 2 and 3 to 0 and 1, then 1 to 0
-#pragma unroll
-      for (int half = 2; half >= 1; half >>= 1) {
-        f32x4* const sh = reinterpret_cast<f32x4*>(sh_ring) + (wave & (half - 1)) * (RB * NF * kWave) + lane;
-        if (wave >= half && wave < 2 * half) {
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-            for (int f = 0; f < NF; ++f) sh[(rb * NF + f) * kWave] = w.o[f][rb];
-        }
-        __syncthreads();
-        if (wave < half) {
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-            for (int f = 0; f < NF; ++f) w.o[f][rb] += sh[(rb * NF + f) * kWave];
-        }
-        __syncthreads();
-      }
-    }
+    if constexpr (MODE == KEYS) w.join(reinterpret_cast<f32x4*>(sh_ring), sh_m, sh_l);
     if (MODE == ROWS || wave == 0) {
-      if (whole) {
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          f32x4 o[NF];
-#pragma unroll
-          for (int f = 0; f < NF; ++f) o[f] = w.o[f][rb];
-          write_part<D, NF, T>(a, p.b, p.head, node0, row0 + rb * 16, rows, 0, o, w.m[rb], w.l[rb]);
-        }
-      } else {
-        // the first piece of the group's run, or its last one
-        const long slot = (static_cast<long>(group) * 2 + (u == unit0 ? 0 : 1)) * (MODE == ROWS ? 4 : 1) + (MODE == ROWS ? wave : 0);
-        const Piece<D, RB> piece(a.partial, slot);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          if (lane < 16) {
-            piece.reference(rb * 16 + r) = w.m[rb];
-            piece.sum(rb * 16 + r) = w.l[rb];
-          }
-#pragma unroll
-          for (int f = 0; f < NF; ++f) piece.part(rb, f, lane) = w.o[f][rb];
-        }
-      }
+      if (whole) w.write(a, p.b, p.head, node0, row0, rows);
+      else  // the first piece of the group's run, or its last one
+        w.save(Piece<W>(a.partial, (static_cast<long>(group) * 2 + (u == unit0 ? 0 : 1)) * (MODE == ROWS ? GROUP : 1) + (MODE == ROWS ? wave : 0)));
     }
     u += taken;
   }
 }
 
 // Joins the pieces of blocks that were dealt to several work-groups: one work-group for every place where the deal cuts one, of which the
-// first of a block takes it; a wave per 16 rows and quarter of the result's channels, eight pieces at a time under way (it is the latency of
-// these loads that counts: a piece at a time took 8 us where this takes 4).
-template <int D, int RB, typename T, int MODE>
-__global__ void __launch_bounds__(kThreads) merge_kernel(AttnArgs a, u32 groups) {
-  constexpr int NF = D / 16, F = NF / 4, AT_ONCE = D == 256 ? 4 : 8;
+// first of a block takes it; a wave per strip of rows and quarter of the result's channels, several pieces at a time under way (it is the latency of
+// these loads that counts: a piece at a time took 8 us where this takes 4; 16 trees, 100 MB of pieces: 18 us).
+template <typename W> __global__ void __launch_bounds__(kThreads) merge_kernel(AttnArgs a, u32 groups) {
+  constexpr int F = W::kQuarter, AT_ONCE = F > 2 ? 4 : 8;
   Deal deal(a, groups);
   if (deal.whole) return;
   const u32 share = deal.share;
@@ -926,47 +908,44 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(AttnArgs a, u32 groups)
   const u32 first = p.begin / share, last = (p.begin + p.count - 1) / share;
   if (cut != first + 1) return;                       // an earlier cut's
   const int node0 = p.block * a.nodes, rows = min(a.nodes, p.r.n - node0) * a.group;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 16;
-  const int f0 = wave * F;
-  constexpr int STRIPS = MODE == ROWS ? 4 * RB : RB;  // of 16 rows
-  for (int strip = blockIdx.y; strip < STRIPS; strip += gridDim.y) {
-  const int part = MODE == ROWS ? strip / RB : 0, rb = MODE == ROWS ? strip % RB : strip;
-  if (strip * 16 >= rows) break;
-  float m = kFloor, l = 0.0f;
-  f32x4 o[F];
+  const int quarter = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  for (int strip = blockIdx.y; strip < W::kStrips && strip * W::kStripRows < rows; strip += gridDim.y) {
+    const int row = W::strip_row(strip);
+    float m = kFloor, l = 0.0f;
+    f32x4 o[F];
 #pragma unroll
-  for (int f = 0; f < F; ++f) o[f] = f32x4{0, 0, 0, 0};
-  for (u32 x0 = first; x0 <= last; x0 += AT_ONCE) {
-    float pm[AT_ONCE], pl[AT_ONCE];
-    f32x4 po[AT_ONCE][F];
+    for (int f = 0; f < F; ++f) o[f] = f32x4{0, 0, 0, 0};
+    for (u32 x0 = first; x0 <= last; x0 += AT_ONCE) {
+      float pm[AT_ONCE], pl[AT_ONCE];
+      f32x4 po[AT_ONCE][F];
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-      const u32 x = min(x0 + i, last);
-      const u32 second = static_cast<unsigned long long>(x) * share >= p.begin ? 0 : 1;
-      const Piece<D, RB> piece(a.partial, (static_cast<long>(x) * 2 + second) * (MODE == ROWS ? 4 : 1) + part);
-      pm[i] = piece.reference(rb * 16 + r);
-      pl[i] = piece.sum(rb * 16 + r);
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const u32 x = min(x0 + i, last);
+        const u32 second = static_cast<unsigned long long>(x) * share >= p.begin ? 0 : 1;
+        const Piece<W> piece(a.partial, (static_cast<long>(x) * 2 + second) * (W::MODE == ROWS ? W::kGroupWaves : 1) + W::strip_wave(strip));
+        pm[i] = piece.reference(row);
+        pl[i] = piece.sum(row);
 #pragma unroll
-      for (int f = 0; f < F; ++f) po[i][f] = piece.part(rb, f0 + f, lane);
-    }
-    const float before = m;
+        for (int f = 0; f < F; ++f) po[i][f] = piece.part(W::strip_part(strip, quarter, f), lane);
+      }
+      const float before = m;
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) m = fmaxf(m, pm[i]);
-    const float shrink = __builtin_amdgcn_exp2f(before - m);
-    l *= shrink;
+      for (int i = 0; i < AT_ONCE; ++i) m = fmaxf(m, pm[i]);
+      const float shrink = __builtin_amdgcn_exp2f(before - m);
+      l *= shrink;
 #pragma unroll
-    for (int f = 0; f < F; ++f) o[f] *= shrink;
+      for (int f = 0; f < F; ++f) o[f] *= shrink;
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-      if (x0 + i <= last) {
-        const float weight = __builtin_amdgcn_exp2f(pm[i] - m);
-        l += pl[i] * weight;
+      for (int i = 0; i < AT_ONCE; ++i) {
+        if (x0 + i <= last) {
+          const float weight = __builtin_amdgcn_exp2f(pm[i] - m);
+          l += pl[i] * weight;
 #pragma unroll
-        for (int f = 0; f < F; ++f) o[f] += po[i][f] * weight;
+          for (int f = 0; f < F; ++f) o[f] += po[i][f] * weight;
+        }
       }
     }
-  }
-  write_part<D, F, T>(a, p.b, p.head, node0, strip * 16, rows, f0, o, m, l);
+    W::write_quarter(a, p.b, p.head, node0, strip, rows, quarter, o, m, l);
   }
 }
 
