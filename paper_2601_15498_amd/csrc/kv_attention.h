@@ -29,7 +29,9 @@ constexpr float kFloor = -3.0e38f;    // the reference before the first key that
 constexpr float kSlack = 8.0f;        // how far (in powers of two) scores may pass the reference before it is moved up
 enum { KEYS = 0, ROWS = 1 };          // what the waves of a work-group divide between them
 
-__device__ __forceinline__ float max3(float a, float b, float c) {  // (written out: fmaxf would first quiet each operand)
+// (Written out: fmaxf would first quiet each operand.  The compiler does not wait for a matrix instruction's results in front of it: `a` comes from an
+// operation of its own on the same results.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
   return r;
@@ -309,10 +311,10 @@ template <int D_, int RB, typename T_> struct Narrow {
     bool up = false;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      float t = max3(sc[0][rb][0], sc[0][rb][1], sc[0][rb][2]);
-      t = max3(t, sc[0][rb][3], sc[1][rb][0]);
-      t = max3(t, sc[1][rb][1], sc[1][rb][2]);
-      t = max3(t, sc[1][rb][3], t);
+      float t = fmaxf(sc[0][rb][0], sc[1][rb][0]);
+      t = max3(t, sc[0][rb][1], sc[0][rb][2]);
+      t = max3(t, sc[0][rb][3], sc[1][rb][1]);
+      t = max3(t, sc[1][rb][2], sc[1][rb][3]);
       top[rb] = t * c;
       up |= top[rb] > m[rb] + kSlack;
     }
@@ -625,10 +627,10 @@ template <int D_, typename T_, int WAVES> struct Wide {
         }
       }
     }
-    float top = max3(s[0], s[1], s[2]);
+    float top = fmaxf(s[0], s[1]);
 #pragma unroll
-    for (int i = 3; i < 15; i += 2) top = max3(top, s[i], s[i + 1]);
-    top = max3(top, s[15], top) * c;
+    for (int i = 2; i < 16; i += 2) top = max3(top, s[i], s[i + 1]);
+    top *= c;
     if (__any(top > m + kSlack)) {  // seldom after the first tiles
       if (kAhead) {
         add_values();
