@@ -69,16 +69,16 @@ struct AttnPlan {
   u32 groups;      // work-groups beside each other on the chip
   size_t bytes;    // of pieces
 };
-// Up to 32 rows of bf16 the waves divide the keys: 28 rows over 4 caches of 60 000 - 131 000 tokens take 110 us so, and 165 in blocks of 16.  Beyond, 32
-// rows each, by 8 waves where their blocks hold no more rows than those of 4 (208 rows over long caches: 440 us, by 4 waves 510; but 288 rows over 16
-// caches of 1 024 - 8 191: 181 and 170; 100 rows: 90 and 78).
-// In 32 bits the products take three times as long and 32 rows a third more registers: up to 64 rows 16 at a time are faster (48 rows: 48 us instead of 78;
-// 120 rows: 98 instead of 92).
+// Up to 32 rows of bf16 the waves divide the keys: 28 rows over 4 caches of 60 000 - 131 000 tokens take 106 us so, and 165 in blocks of 16.  Beyond, 32
+// rows each, by 8 waves where their blocks hold no more rows than those of 4 (208 rows over long caches: 410 us, by 4 waves 480; but 288 rows over 16
+// caches of 1 024 - 8 191: 175 and 169; 100 rows: 89 and 77).
+// In 32 bits the products take three times as long and 32 rows a third more registers: up to 80 rows 16 at a time are faster (48 rows: 47 us instead of 71, 80
+// rows: 66 and 77; 120 rows: 97 and 84).
 static AttnPlan attn_plan(int N, int group, int dim, int dtype) {
   const long rows = static_cast<long>(N) * group;
   const bool f32 = dtype == MARS_F32;
   AttnPlan p;
-  p.mode = (f32 ? group <= 16 && rows <= 64 : rows <= 32) ? KEYS : ROWS;
+  p.mode = (f32 ? group <= 16 && rows <= 80 : rows <= 32) ? KEYS : ROWS;
   p.rows = p.mode == KEYS && (f32 || rows <= 16) ? 16 : 32;
   const long four = (rows + kWaves * 32 - 1) / (kWaves * 32);  // blocks of four waves
   p.waves = p.mode == ROWS && four % 2 == 0 && !f32 && dim <= 128 ? 2 * kWaves : kWaves;

@@ -8,14 +8,13 @@
 //
 // Few rows (Narrow, up to 32): the four waves of a work-group take every fourth tile of the same rows and meet in LDS at the end.  Bound by the cache's way from
 // memory: 64 tokens over 500 - 8 192, 304 MB, 73 us, of which in the middle 8.5 TB/s, the rest is the beginning and the end.
-// More (Wide): each of four or eight waves has 32 rows of its own, the values are converted once for all of them.  Bound by what the card may draw: the matrix cores
-// work for half of the clocks, at 1.7 to 2.0 GHz.
+// More (Wide): each of four or eight waves has 32 rows of its own, the values are converted once for all of them.  Bound by the matrix cores and the vector
+// instructions between them, and by the clock that the card keeps meanwhile.
 // The work is dealt out by kv_deal.h: a work-group takes a run of tiles that may begin and end inside a block of rows; what it has of such a
 // block goes to the workspace, and merge_kernel joins the pieces.
 #pragma once
 
 #include <type_traits>
-#include <utility>
 
 #include "kv_deal.h"
 #include "kv_format.h"
@@ -53,17 +52,13 @@ template <int TERMS> __device__ __forceinline__ void split_pair(float a, float b
   }
 }
 
-// f(0), f(1), .. f(N - 1), each with its constant.
-template <int... I, typename F> __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F f) { (f(std::integral_constant<int, I>{}), ...); }
-template <int N, typename F> __device__ __forceinline__ void each(F f) { each_of(std::make_integer_sequence<int, N>{}, f); }
-
 // Two keys' values of the same channel beside each other: the low halves of two conversions, or the high ones.
 __device__ __forceinline__ u32 low_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
 // The queries, as the first product's second operand, are bf16 rows as they are; fp32 rows are three bf16 terms, as the probabilities then are (one term for bf16
 // rows, whose results are rounded to as many bits).  The matrix cores also take codes and scales as they are, by queries of 8 bits: two such terms hold a bf16 number,
-// and the conversion of the keys falls away (395 us instead of 440 with long caches, nothing with few rows).  But products of one instruction 2^16 below the
+// and the conversion of the keys falls away (a tenth of the time with long caches, nothing with few rows).  But products of one instruction 2^16 below the
 // largest are dropped there, and scores of 100 came out 1e-3 off; so it is not used.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -429,11 +424,11 @@ template <int D_, int RB, typename T_> struct Narrow {
 //   scores    first operand: key r of the tile, half of its channels.  The lane ends up with the scores of keys 8a + 4h + i, i < 4, for its query --
 //   values    -- which are eight keys each of the second product's two steps: keys 16t + 4h .. + 3 and 8 more on.  Its first operand: the same keys of D/32 channels.
 // The waves of a work-group go through the tiles together, each converts the values of 16 keys of the next step for all of them, and waits for the others once per
-// step (64 keys for four waves, 128 for eight, of which one work-group fills a compute unit; two of four end 20% apart, as one is served first throughout).  With the
-// scores a tile ahead, the second product a tile behind and the exponentials between them there is always something to issue.
-// 4 trees of 208 rows over 60 000 - 131 000 tokens: 440 us (0.78 PFLOP/s, 0.84 with the rows that fill up the last wave's 32; a large library product reaches
-// 1.2), by work-groups of four waves 510.  16 trees of 240 rows over 1 024 - 8 191: 110 us, by four 118.  The matrix cores are busy for half of the clocks; finer
-// interleaving, priorities and a deeper ring changed nothing, and the clock falls to 1.7 - 2.0 GHz meanwhile: it is the power that bounds it.
+// step (64 keys for four waves, 128 for eight, of which one work-group fills a compute unit; two of four end 20% apart, as one is served first throughout).
+// 4 trees of 208 rows over 60 000 - 131 000 tokens: 410 us (0.83 PFLOP/s, 0.9 with the rows that fill up the last wave's 32; a large library product reaches
+// 1.2), by work-groups of four waves 480, by waves of 64 rows, one per SIMD, 580.  16 trees of 240 rows over 1 024 - 8 191: 107 us, by four 118.  The matrix
+// cores are busy for half of the clocks, of which there are 1.7 to 2.0 GHz under this load.  Scores a tile ahead, the exponentials laid between the matrix instructions,
+// priorities and a deeper ring changed nothing or cost a little.
 template <int D> struct Keys32 {
   u32 k[D / 64][4], ks[D / 64];  // 32 channels each, 64 s + 32 h
   Keys32() = default;
@@ -472,19 +467,28 @@ template <int D> struct Values32 {
       vs[o] = n >= 4 ? vs[o] : n <= 0 ? 0 : vs[o] & ((1u << (8 * n)) - 1);
     }
   }
-  // f(block, fragment) for blocks 2 BYTE and 2 BYTE + 1 of the C: channel C r + block.
-  template <int BYTE, typename F> __device__ __forceinline__ void pair(F f) const {
+  // f(block, fragment) for the C blocks: channel C r + block.
+  template <typename F> __device__ __forceinline__ void each(F f) const {
     const u32 shift = D == 64 ? (threadIdx.x & 3) * 8 : D == 128 ? (threadIdx.x & 1) * 16 : 0;
     u32 w[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) w[j] = v[j / 4][j % 4] >> shift;
     const u32 s[8] = {scale_at<0>(vs[0]), scale_at<1>(vs[0]), scale_at<2>(vs[0]), scale_at<3>(vs[0]),
                       scale_at<0>(vs[1]), scale_at<1>(vs[1]), scale_at<2>(vs[1]), scale_at<3>(vs[1])};
-    u32 y[8];
+    auto pair = [&](auto byte) {
+      constexpr int BYTE = decltype(byte)::value;
+      u32 y[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = decode<BYTE>(w[j], s[j]);
-    f(2 * BYTE, as_bf16x8(low_halves(y[0], y[1]), low_halves(y[2], y[3]), low_halves(y[4], y[5]), low_halves(y[6], y[7])));
-    f(2 * BYTE + 1, as_bf16x8(high_halves(y[0], y[1]), high_halves(y[2], y[3]), high_halves(y[4], y[5]), high_halves(y[6], y[7])));
+      for (int j = 0; j < 8; ++j) y[j] = decode<BYTE>(w[j], s[j]);
+      f(2 * BYTE, as_bf16x8(low_halves(y[0], y[1]), low_halves(y[2], y[3]), low_halves(y[4], y[5]), low_halves(y[6], y[7])));
+      f(2 * BYTE + 1, as_bf16x8(high_halves(y[0], y[1]), high_halves(y[2], y[3]), high_halves(y[4], y[5]), high_halves(y[6], y[7])));
+    };
+    pair(std::integral_constant<int, 0>{});
+    if constexpr (C > 2) pair(std::integral_constant<int, 1>{});
+    if constexpr (C > 4) {
+      pair(std::integral_constant<int, 2>{});
+      pair(std::integral_constant<int, 3>{});
+    }
   }
 };
 
@@ -503,12 +507,16 @@ template <int D, typename T> struct Queries32 {
       for (int k = 0; k < TERMS; ++k) q[k][s] = as_bf16x8(t[0][k], t[1][k], t[2][k], t[3][k]);
     }
   }
-  static constexpr int kSteps = S * TERMS;
-  __device__ __forceinline__ void step(int i, f32x16& sc, const Keys32<D>& x) const {
-    const int s = i / TERMS, t = TERMS - 1 - i % TERMS;
-    const u32 scale = scale_at<0>(x.ks[s / 4]), w = x.k[s / 4][s % 4];
-    const bf16x8 k = as_bf16x8(decode<0>(w, scale), decode<1>(w, scale), decode<2>(w, scale), decode<3>(w, scale));
-    sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[t][s], i == 0 ? f32x16{} : sc, 0, 0, 0);
+  __device__ __forceinline__ f32x16 scores(const Keys32<D>& x) const {
+    f32x16 sc = {};
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const u32 scale = scale_at<0>(x.ks[s / 4]), w = x.k[s / 4][s % 4];
+      const bf16x8 k = as_bf16x8(decode<0>(w, scale), decode<1>(w, scale), decode<2>(w, scale), decode<3>(w, scale));
+#pragma unroll
+      for (int t = TERMS - 1; t >= 0; --t) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[t][s], sc, 0, 0, 0);
+    }
+    return sc;
   }
 };
 
@@ -544,14 +552,8 @@ template <int D_, typename T_, int WAVES> struct Wide {
   static constexpr int C = D / 32;              // blocks of 32 channels of the result
   static constexpr int kParts = 4 * C;          // four numbers of a lane each
   static constexpr int TERMS = std::is_same<T, float>::value ? 3 : 1;
-  static constexpr bool kAhead = TERMS == 1;    // scores a tile ahead, the second product a tile behind (three terms' operands leave no registers for it)
-  static constexpr int kNext = kAhead ? 2 : 1;  // how far in front of a tile keys are loaded
-  using Q = Queries32<D, T>;
-  Q q;
-  f32x16 sc[kAhead ? 2 : 1];                    // scores of this tile and the next
+  Queries32<D, T> q;
   Keys32<D> next;                               // of the next tile
-  u32 p[TERMS][2][4];                           // of the tile before: probabilities, in terms, two steps of the product with
-  u32x4 v[2 * C];                               // its values
   f32x16 o[C];                                  // [block][i]: channel C (8 (i/4) + 4h + i%4) + block
   float m, l;
   int node;                                     // of this lane's row; < 0: no row
@@ -565,56 +567,23 @@ template <int D_, typename T_, int WAVES> struct Wide {
     m = kFloor;
     l = 0.0f;
 #pragma unroll
-    for (int k = 0; k < C; ++k) {
-      o[k] = f32x16{};
-      v[k] = v[C + k] = u32x4{0, 0, 0, 0};
-    }
-    clear_before();
+    for (int k = 0; k < C; ++k) o[k] = f32x16{};
   }
   // A step's values as operands, to `values` [tile][2 C][64]: 16 keys' by each wave.  `tiles`: the step's, keys t0 ..
-  __device__ __forceinline__ static Values32<D> sixteen(const uint8_t* tiles, const u32* sh_bad, int t0, int end) {
+  __device__ __forceinline__ static void convert(const uint8_t* tiles, u32x4* values, const u32* sh_bad, int t0, int end) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const u32 bad = __builtin_amdgcn_readfirstlane(sh_bad[wave / 2]) >> (wave % 2 * 2);
     t0 += wave * 16;
     Values32<D> x(tiles + wave / 2 * Tile<D>::kBytes, wave % 2);
     if (t0 + 16 > end || (bad & 3)) x.cut(end - t0, bad);
-    return x;
+    u32x4* const at = values + wave * C * kWave + threadIdx.x % kWave;
+    x.each([&](int k, bf16x8 v) { at[k * kWave] = __builtin_bit_cast(u32x4, v); });
   }
-  template <int I> __device__ __forceinline__ static void convert(const Values32<D>& x, u32x4* values) {  // part I of C / 2
-    u32x4* const at = values + threadIdx.x / kWave * C * kWave + threadIdx.x % kWave;
-    if constexpr (I < C / 2) x.template pair<I>([&](int k, bf16x8 v) { at[k * kWave] = __builtin_bit_cast(u32x4, v); });
-  }
-  __device__ __forceinline__ void first_product(f32x16& to) {
-#pragma unroll
-    for (int i = 0; i < Q::kSteps; ++i) q.step(i, to, next);
-  }
-  __device__ __forceinline__ void begin(const uint8_t* tiles) {
-    next = Keys32<D>(tiles);
-    if (!kAhead) return;
-    first_product(sc[0]);
-    next = Keys32<D>(tiles + Tile<D>::kBytes);
-  }
-  __device__ __forceinline__ void clear_before() {
-#pragma unroll
-    for (int i = 0; i < TERMS * 8; ++i) p[i / 8][i % 8 / 4][i % 4] = 0;
-  }
-  // The second product of the tile before, in kAdds steps.
-  static constexpr int kAdds = 2 * C * TERMS;
-  __device__ __forceinline__ void add(int i) {
-    const int t = i / (C * TERMS), k = i % (C * TERMS) / TERMS, x = TERMS - 1 - i % TERMS;
-    o[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[t * C + k]), as_bf16x8(p[x][t][0], p[x][t][1], p[x][t][2], p[x][t][3]), o[k], 0, 0, 0);
-  }
-  __device__ __forceinline__ void add_values() {
-#pragma unroll
-    for (int i = 0; i < kAdds; ++i) add(i);
-  }
-  // A tile (as Narrow::tile says), an even or an odd one, its values as operands at `values`; in the meantime f(0), f(1) ...  kAhead: on the matrix cores are the next
-  // tile's scores and the product with the values of the tile before.  `after`: the tile whose keys are loaded meanwhile.
-  template <int I, typename F>
-  __device__ __forceinline__ void tile(const AttnArgs& a, const uint8_t* after, const u32x4* values, u32 bad, int b, int len, int n, int t0, F f) {
+  __device__ __forceinline__ void begin(const uint8_t* tile) { next = Keys32<D>(tile); }
+  // A tile (as Narrow::tile says), its values as operands at `values`; the next one is at `after`.
+  __device__ __forceinline__ void tile(const AttnArgs& a, const uint8_t* after, const u32x4* values, u32 bad, int b, int len, int n, int t0) {
     const float c = a.scale_log2;
-    f32x16& s = sc[kAhead ? I : 0];
-    if constexpr (!kAhead) first_product(s);
+    f32x16 s = q.scores(next);
     if (t0 + kTile > len || bad) {
       const int h = threadIdx.x % kWave / 32;
 #pragma unroll
@@ -632,10 +601,6 @@ template <int D_, typename T_, int WAVES> struct Wide {
     for (int i = 2; i < 16; i += 2) top = max3(top, s[i], s[i + 1]);
     top *= c;
     if (__any(top > m + kSlack)) {  // seldom after the first tiles
-      if (kAhead) {
-        add_values();
-        clear_before();
-      }
       top = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
       const float shrink = __builtin_amdgcn_exp2f(m - top);
       m = top;
@@ -643,55 +608,31 @@ template <int D_, typename T_, int WAVES> struct Wide {
 #pragma unroll
       for (int k = 0; k < C; ++k) o[k] *= shrink;
     }
-    __builtin_amdgcn_sched_barrier(0);
-    auto weigh = [&](int j, u32 (&to)[TERMS][2][4]) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * j], c, -m)), e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * j + 1], c, -m));
+    next = Keys32<D>(after);  // (5% faster here than in front of the branches)
+    u32 p[TERMS][2][4];  // probabilities, in terms, of the two steps of the product with the values
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * i], c, -m)), e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], c, -m));
       l += e0 + e1;
       u32 x[TERMS];
       split_pair<TERMS>(e0, e1, x);
 #pragma unroll
-      for (int k = 0; k < TERMS; ++k) to[k][j / 4][j % 4] = x[k];
-    };
+      for (int k = 0; k < TERMS; ++k) p[k][i / 4][i % 4] = x[k];
+    }
+    u32x4 v[2 * C];
     auto load = [&](int k) { v[k] = values[k * kWave + threadIdx.x % kWave]; };
-    if constexpr (kAhead) {
-      // Between two matrix instructions what the vector port can do while the first runs.
-      constexpr int kAll = Q::kSteps + kAdds;
-      u32 e[TERMS][2][4];
-      each<Q::kSteps>([&](auto i) {
-        q.step(i, sc[1 - I], next);
+    load(0);
+    load(1);
 #pragma unroll
-        for (int j = i * 8 / kAll; j < (i + 1) * 8 / kAll; ++j) weigh(j, e);
-        f(i);
-        __builtin_amdgcn_sched_barrier(0);
-      });
-      next = Keys32<D>(after);
-      each<kAdds>([&](auto i) {
-        add(i);
+    for (int i = 0; i < 2 * C; ++i) {
+      const int t = i / C, k = i % C;
+      if (i + 2 < 2 * C) load(i + 2);
 #pragma unroll
-        for (int j = (Q::kSteps + i) * 8 / kAll; j < (Q::kSteps + i + 1) * 8 / kAll; ++j) weigh(j, e);
-        load(i);
-        __builtin_amdgcn_sched_barrier(0);
-      });
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[0][i / 4][i % 4] = e[0][i / 4][i % 4];
-    } else {
-      load(0);
-      load(1);
-      next = Keys32<D>(after);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) weigh(j, p);
-      each<C / 2>(f);
-      each<kAdds>([&](auto i) {
-        add(i);
-        if constexpr (i % TERMS == TERMS - 1 && i / TERMS + 2 < 2 * C) load(i / TERMS + 2);
-        __builtin_amdgcn_sched_barrier(0);
-      });
+      for (int x = TERMS - 1; x >= 0; --x)
+        o[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v[i]), as_bf16x8(p[x][t][0], p[x][t][1], p[x][t][2], p[x][t][3]), o[k], 0, 0, 0);
     }
   }
-  __device__ __forceinline__ void finish() {
-    if (kAhead) add_values();
-    l += __shfl_xor(l, 32);
-  }
+  __device__ __forceinline__ void finish() { l += __shfl_xor(l, 32); }
   __device__ __forceinline__ f32x4 part(int i) const { return f32x4{o[i / 4][i % 4 * 4], o[i / 4][i % 4 * 4 + 1], o[i / 4][i % 4 * 4 + 2], o[i / 4][i % 4 * 4 + 3]}; }
   __device__ __forceinline__ void write(const AttnArgs& a, int b, int head, int node0, int row0, int rows) const {
 #pragma unroll
@@ -846,24 +787,19 @@ __global__ void __launch_bounds__(W::kGroupWaves * kWave, kPerUnit<W> * W::kGrou
         if (mine) issue_behind(unit, at);
       };
       auto step = [&](const uint8_t* now, const u32* bad, const uint8_t* then, const u32* bad_then) {
-        const auto x = W::sixteen(then, bad_then, t0 + TILES * kTile, end);
-        each<TILES>([&](auto number) {
-          constexpr int I = decltype(number)::value;
-          auto convert = [&](auto part) {
-            if constexpr (I == 0) W::template convert<decltype(part)::value>(x, there);
-          };
+        W::convert(then, there, bad_then, t0 + TILES * kTile, end);
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
           if (t0 < limit)
-            w.template tile<I % 2>(a, I + W::kNext < TILES ? now + (I + W::kNext) * X::kBytes : then + (I + W::kNext - TILES) * X::kBytes, here + I * (D / 16) * kWave,
-                                   __builtin_amdgcn_readfirstlane(bad[I]), p.b, len, n, t0, convert);
-          else each<D / 64>(convert);
+            w.tile(a, i + 1 < TILES ? now + (i + 1) * X::kBytes : then, here + i * (D / 16) * kWave, __builtin_amdgcn_readfirstlane(bad[i]), p.b, len, n, t0);
           t0 += kTile;
-        });
+        }
         u32x4* const done = here;
         here = there;
         there = done;
       };
       next_step(0, 0, 0);
-      each<D / 64>([&, x = W::sixteen(sh_ring, sh_bad[0], t0, end)](auto part) { W::template convert<decltype(part)::value>(x, here); });
+      W::convert(sh_ring, here, sh_bad[0], t0, end);
       w.begin(sh_ring);
       for (int unit = 0; unit < units; ++unit) {
         const uint8_t* const now = sh_ring + stage * kWaves * X::kBytes;
