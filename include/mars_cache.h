@@ -48,7 +48,7 @@ enum {
   MARS_KV_NOT_EMPTY    = 5  /* the target of a fork holds pages */
 };
 
-/* Most requests per call, and query rows per request under a mask. */
+/* Most requests per call. */
 #define MARS_KV_MAX_REQUESTS 4096
 
 /* The cache (a HOST struct; the pointers in it are device pointers).  A call that does not name a table may be given NULL for it. */

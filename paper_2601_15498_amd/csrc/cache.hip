@@ -58,8 +58,11 @@ template <typename F> static int by_type(int dtype, F f) { return dtype == MARS_
 
 static int row_octets(int N) { return (N + 6) / 8 + 1; }  // octets that N positions can touch
 
+// Work-groups of a commit: 256 paths in 32 layers and 8 heads take 40 us by about 2 048, 47 by 512, 69 by 16 384.
 constexpr int kCommitGroups = 2048;
-constexpr int kPlanFewPages = 16384;  // four steps of the search
+// Pools of up to this many pages are searched for free ones by 256 threads (four steps): one request's two children 16.8 us, by 1 024 threads 18.5; in a pool of 60 000
+// pages 107 and 103.
+constexpr int kPlanFewPages = 16384;
 
 // ---------------------------------------------------------------- attention: how the work is laid out
 struct AttnPlan {
@@ -89,8 +92,14 @@ static AttnPlan attn_plan(int N, int group, int dim, int dtype) {
   p.bytes = align_up(static_cast<size_t>(p.groups) * 2 * (p.mode == ROWS ? p.waves : 1) * piece);
   return p;
 }
-// Blocks of so few units (as far as the caller says) are not cut: their pieces would have to be joined by a second kernel.
-constexpr int kWholeUnits = 8;
+// Blocks of up to this many units (as far as the caller says) are not cut: their pieces would have to be joined, by a second kernel.  One token, 8 heads, 1 021
+// tokens: 12 us, cut 15; 1 500: 15 and 12.5.  Where there are blocks enough for half the compute units, and each is a few rows of bf16 (light), cutting wins less: 32 times one token over
+// 1 900 - 2 000, 256 blocks: 19 us, cut 28; 8 times, 64 blocks: 18.6 and 17.7.
+static int whole_units(bool light, long blocks) { return light && blocks >= 128 ? 16 : 8; }
+// The same where the lengths decide (the second kernel runs in any case then), in units beyond an even share: 64 times one token over 500 - 2 000 26 us with
+// 12, 32 with 8; one over 1 500 18 and 13.  With more rows a unit takes longer: 8 trees of 240 rows over 1 000 - 1 900 72 us with 12, 46 with 8, 46 with 0; 32 such
+// trees 80, 80 and 94.
+static u32 join_cost(bool light, long blocks) { return light && blocks >= 128 ? 12 : 8; }
 
 template <typename W> static int launch_attention(u32 groups, const AttnArgs& a, hipStream_t stream) {
   static_assert(Piece<W>::kFloats == 2 * W::kRows + W::kRows * W::D, "as attn_plan counts them");
@@ -213,7 +222,9 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
   const long most_len = static_cast<long>(c.width) << c.log_page, blocks = static_cast<long>(B) * c.heads * ((N + p.nodes - 1) / p.nodes);
   const double units = static_cast<double>(blocks) * ((most_len + N + 3 * kUnit) / kUnit);  // at most; counted in 32 bits
   if (units > 4.0e9) return MARS_ERR_ARG;
-  a.whole = ((max_len && max_len < most_len ? max_len : most_len) + N + kUnit - 1) / kUnit <= kWholeUnits;
+  const bool light = p.mode == KEYS && dtype == MARS_BF16;
+  a.whole = ((max_len && max_len < most_len ? max_len : most_len) + N + kUnit - 1) / kUnit <= whole_units(light, blocks);
+  a.join_cost = join_cost(light, blocks);
   const double wanted = a.whole ? (blocks < (1 << 20) ? blocks : 1 << 20) : units < p.groups ? units : p.groups;
   const u32 groups = (static_cast<u32>(wanted) + 7) / 8 * 8;  // dealt out die by die
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);

@@ -718,9 +718,11 @@ __global__ void __launch_bounds__(W::kGroupWaves * kWave, kPerUnit<W> * W::kGrou
       if (n < a.N) clear_rows<typename W::T, D>(a, b, n);
     }
   Deal deal(a, gridDim.x);
+  if (deal.total == 0) return;
   const u32 share = deal.share;
-  // neighbours in the deal on the same die (block index mod 8)
-  const u32 per_die = gridDim.x >> 3;
+  // neighbours in the deal on the same die (block index mod 8), all dies alike
+  const u32 per_die = ((deal.total + share - 1) / share + 7) >> 3;
+  if (blockIdx.x >> 3 >= per_die) return;
   const u32 group = (blockIdx.x & 7) * per_die + (blockIdx.x >> 3);
   const unsigned long long my_begin = static_cast<unsigned long long>(group) * share;
   if (my_begin >= deal.total) return;
@@ -836,7 +838,7 @@ __global__ void __launch_bounds__(W::kGroupWaves * kWave, kPerUnit<W> * W::kGrou
 template <typename W> __global__ void __launch_bounds__(kThreads) merge_kernel(AttnArgs a, u32 groups) {
   constexpr int F = W::kQuarter, AT_ONCE = F > 2 ? 4 : 8;
   Deal deal(a, groups);
-  if (deal.whole) return;
+  if (deal.whole || deal.total == 0) return;
   const u32 share = deal.share;
   const u32 cut = blockIdx.x + 1;
   const unsigned long long at = static_cast<unsigned long long>(cut) * share;

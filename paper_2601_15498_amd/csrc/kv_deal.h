@@ -27,7 +27,8 @@ struct AttnArgs {
   float scale_log2;
   int B, N, q_heads, group, words;
   int nodes;    // of a block of rows
-  bool whole;   // the deal gives out whole items
+  u32 join_cost; // how many units more than its share a work-group takes rather than have blocks cut
+  bool whole;    // the deal gives out whole items in any case
 };
 
 // ---------------------------------------------------------------- the deal
@@ -75,10 +76,8 @@ __device__ __forceinline__ u32 wave_max(u32 v) {
              max(static_cast<u32>(__builtin_amdgcn_readlane(v, 47)), static_cast<u32>(__builtin_amdgcn_readlane(v, 63))));
 }
 // What a work-group's share of the units comes to, and a place in the deal, kept by every wave for itself: 64 requests at a time, one per lane.
-// Where no work-group gets much more by it (kJoinCost), whole items are given out and none is cut: then an item counts as two, one for each
+// Where no work-group gets much more by it (join_cost units), whole items are given out and none is cut: then an item counts as two, one for each
 // of its blocks.
-constexpr u32 kJoinCost = 8;  // units; two prompts of 2 048, every pair of blocks with a work-group of its own: 50 units instead of 45, and the
-                              // pieces' 134 MB neither written nor read
 struct Deal {
   const AttnArgs& a;
   Request mine;       // of request first + lane
@@ -112,7 +111,7 @@ struct Deal {
     }
     share = (total + groups - 1) / groups;
     const u32 each = (items + groups - 1) / groups;
-    whole = a.whole || each * most <= share + kJoinCost;
+    whole = a.whole || each * most <= share + a.join_cost;
     if (whole) {
       share = 2 * each;
       total = 2 * items;
