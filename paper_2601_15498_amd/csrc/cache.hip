@@ -101,6 +101,11 @@ static int whole_units(bool light, long blocks) { return light && blocks >= 128 
 // trees 80, 80 and 94.
 static u32 join_cost(bool light, long blocks) { return light && blocks >= 128 ? 12 : 8; }
 
+// Units that a work-group takes at least: with two, pieces are half as many to join.  One token over 4 000: 14.7 us instead of 17.9, 8 over 1 500 14.9 and 19.0, 2 trees
+// of 240 rows over 1 900 36 and 41; but 2 of 28 rows over 1 000 - 1 900 23.6 and 19.0, 2 of 7 in fp32 16.4 and 14.6, whose units take longer and whose pieces are
+// small.  (Three: one token over 2 000 15.2 instead of 12.2.)
+static u32 least_share(const AttnPlan& p, int dtype) { return p.mode == KEYS && (dtype == MARS_F32 || p.rows == 32) ? 1 : 2; }
+
 template <typename W> static int launch_attention(u32 groups, const AttnArgs& a, hipStream_t stream) {
   static_assert(Piece<W>::kFloats == 2 * W::kRows + W::kRows * W::D, "as attn_plan counts them");
   if (a.c.log_page >= 5) hipLaunchKernelGGL((attention_kernel<W, true>), dim3(groups), dim3(W::kGroupWaves * kWave), 0, stream, a);
@@ -225,6 +230,7 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
   const bool light = p.mode == KEYS && dtype == MARS_BF16;
   a.whole = ((max_len && max_len < most_len ? max_len : most_len) + N + kUnit - 1) / kUnit <= whole_units(light, blocks);
   a.join_cost = join_cost(light, blocks);
+  a.least_share = least_share(p, dtype);
   const double wanted = a.whole ? (blocks < (1 << 20) ? blocks : 1 << 20) : units < p.groups ? units : p.groups;
   const u32 groups = (static_cast<u32>(wanted) + 7) / 8 * 8;  // dealt out die by die
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);

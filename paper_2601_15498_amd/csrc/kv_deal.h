@@ -27,8 +27,9 @@ struct AttnArgs {
   float scale_log2;
   int B, N, q_heads, group, words;
   int nodes;    // of a block of rows
-  u32 join_cost; // how many units more than its share a work-group takes rather than have blocks cut
-  bool whole;    // the deal gives out whole items in any case
+  u32 least_share;  // units that a work-group takes at least
+  u32 join_cost;    // how many units more than its share it takes rather than have blocks cut
+  bool whole;       // the deal gives out whole items in any case
 };
 
 // ---------------------------------------------------------------- the deal
@@ -109,7 +110,7 @@ struct Deal {
       total += wave_sum(in ? mine.items(a) * mine.per : 0);
       most = max(most, wave_max(in && mine.items(a) ? mine.per : 0));
     }
-    share = (total + groups - 1) / groups;
+    share = total ? max((total + groups - 1) / groups, a.least_share) : 0;
     const u32 each = (items + groups - 1) / groups;
     whole = a.whole || each * most <= share + a.join_cost;
     if (whole) {
