@@ -60,8 +60,8 @@ static int row_octets(int N) { return (N + 6) / 8 + 1; }  // octets that N posit
 
 // Work-groups of a commit: 256 paths in 32 layers and 8 heads take 40 us by about 2 048, 47 by 512, 69 by 16 384.
 constexpr int kCommitGroups = 2048;
-// Pools of up to this many pages are searched for free ones by 256 threads (four steps): one request's two children 16.8 us, by 1 024 threads 18.5; in a pool of 60 000
-// pages 107 and 103.
+// Pools of up to this many pages are searched for free ones by 256 threads (four steps): one request's two children 16.8 us, by 1 024 threads 18.5;
+// in a pool of 60 000 pages 107 and 103.
 constexpr int kPlanFewPages = 16384;
 
 // ---------------------------------------------------------------- attention: how the work is laid out
@@ -92,18 +92,18 @@ static AttnPlan attn_plan(int N, int group, int dim, int dtype) {
   p.bytes = align_up(static_cast<size_t>(p.groups) * 2 * (p.mode == ROWS ? p.waves : 1) * piece);
   return p;
 }
-// Blocks of up to this many units (as far as the caller says) are not cut: their pieces would have to be joined, by a second kernel.  One token, 8 heads, 1 021
-// tokens: 12 us, cut 15; 1 500: 15 and 12.5.  Where there are blocks enough for half the compute units, and each is a few rows of bf16 (light), cutting wins less: 32 times one token over
-// 1 900 - 2 000, 256 blocks: 19 us, cut 28; 8 times, 64 blocks: 18.6 and 17.7.
+// Blocks of up to this many units (as far as the caller says) are not cut: their pieces would have to be joined, by a second kernel.  One token, 8
+// heads, 1 021 tokens: 12 us, cut 15; 1 500: 15 and 12.5.  Where there are blocks enough for half the compute units, and each is a few rows of bf16
+// (light), cutting wins less: 32 times one token over 1 900 - 2 000, 256 blocks: 19 us, cut 28; 8 times, 64 blocks: 18.6 and 17.7.
 static int whole_units(bool light, long blocks) { return light && blocks >= 128 ? 16 : 8; }
 // The same where the lengths decide (the second kernel runs in any case then), in units beyond an even share: 64 times one token over 500 - 2 000 26 us with
 // 12, 32 with 8; one over 1 500 18 and 13.  With more rows a unit takes longer: 8 trees of 240 rows over 1 000 - 1 900 72 us with 12, 46 with 8, 46 with 0; 32 such
 // trees 80, 80 and 94.
 static u32 join_cost(bool light, long blocks) { return light && blocks >= 128 ? 12 : 8; }
 
-// Units that a work-group takes at least: with two, pieces are half as many to join.  One token over 4 000: 14.7 us instead of 17.9, 8 over 1 500 14.9 and 19.0, 2 trees
-// of 240 rows over 1 900 36 and 41; but 2 of 28 rows over 1 000 - 1 900 23.6 and 19.0, 2 of 7 in fp32 16.4 and 14.6, whose units take longer and whose pieces are
-// small.  (Three: one token over 2 000 15.2 instead of 12.2.)
+// Units that a work-group takes at least: with two, pieces are half as many to join.  One token over 4 000: 14.7 us instead of 17.9, 8 over 1 500
+// 14.9 and 19.0, 2 trees of 240 rows over 1 900 36 and 41; but 2 of 28 rows over 1 000 - 1 900 23.6 and 19.0, 2 of 7 in fp32 16.4 and 14.6, whose
+// units take longer and whose pieces are small.  (Three: one token over 2 000 15.2 instead of 12.2.)
 static u32 least_share(const AttnPlan& p, int dtype) { return p.mode == KEYS && (dtype == MARS_F32 || p.rows == 32) ? 1 : 2; }
 
 template <typename W> static int launch_attention(u32 groups, const AttnArgs& a, hipStream_t stream) {

@@ -56,10 +56,10 @@ template <int TERMS> __device__ __forceinline__ void split_pair(float a, float b
 __device__ __forceinline__ u32 low_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// The queries, as the first product's second operand, are bf16 rows as they are; fp32 rows are three bf16 terms, as the probabilities then are (one term for bf16
-// rows, whose results are rounded to as many bits).  The matrix cores also take codes and scales as they are, by queries of 8 bits: two such terms hold a bf16 number,
-// and the conversion of the keys falls away (a tenth of the time with long caches, nothing with few rows).  But products of one instruction 2^16 below the
-// largest are dropped there, and scores of 100 came out 1e-3 off; so it is not used.
+// The queries, as the first product's second operand, are bf16 rows as they are; fp32 rows are three bf16 terms, as the probabilities then are (one
+// term for bf16 rows, whose results are rounded to as many bits).  The matrix cores also take codes and scales as they are, by queries of 8 bits: two
+// such terms hold a bf16 number, and the conversion of the keys falls away (a tenth of the time with long caches, nothing with few rows).  But
+// products of one instruction 2^16 below the largest are dropped there, and scores of 100 came out 1e-3 off; so it is not used.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // Which of the keys first .. first + 7 (numbered from the first node on; committed ones are < 0) row `node` of n nodes sees.  `only`: its mask, if that
