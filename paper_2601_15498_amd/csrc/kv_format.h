@@ -61,22 +61,24 @@ __device__ __forceinline__ uint8_t* head_of(const Cache& c, size_t layer_offset,
   return c.pool + layer_offset + static_cast<size_t>(page) * c.page_bytes + static_cast<size_t>(head) * c.blk;
 }
 
-// Eight channels of a row, widened.
+// Eight channels of a row: as they lie in memory, and widened.
 struct Eight { float x[8]; };
-__device__ __forceinline__ Eight load_eight(const float* p) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
-  return {{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
-}
-__device__ __forceinline__ Eight load_eight(const bf16_t* p) {
-  const u32x4 a = *reinterpret_cast<const u32x4*>(p);
+template <typename T> struct Raw;
+template <> struct Raw<float> { f32x4 a, b; };
+template <> struct Raw<bf16_t> { u32x4 a; };
+__device__ __forceinline__ Raw<float> load_raw(const float* p) { return {*reinterpret_cast<const f32x4*>(p), *reinterpret_cast<const f32x4*>(p + 4)}; }
+__device__ __forceinline__ Raw<bf16_t> load_raw(const bf16_t* p) { return {*reinterpret_cast<const u32x4*>(p)}; }
+__device__ __forceinline__ Eight widen(const Raw<float>& r) { return {{r.a[0], r.a[1], r.a[2], r.a[3], r.b[0], r.b[1], r.b[2], r.b[3]}}; }
+__device__ __forceinline__ Eight widen(const Raw<bf16_t>& r) {
   Eight e;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    e.x[2 * i] = __uint_as_float(a[i] << 16);
-    e.x[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
+    e.x[2 * i] = __uint_as_float(r.a[i] << 16);
+    e.x[2 * i + 1] = __uint_as_float(r.a[i] & 0xFFFF0000u);
   }
   return e;
 }
+template <typename T> __device__ __forceinline__ Eight load_eight(const T* p) { return widen(load_raw(p)); }
 // Largest magnitude's bits; with a NaN or an infinity among them 0x7F800000 or more.
 __device__ __forceinline__ u32 top_bits(const Eight& e) {
   u32 m = 0;

@@ -22,7 +22,7 @@ __device__ __forceinline__ void report(int32_t* status, int b, int value) {
 // An item is eight positions beside each other (an octet: the unit of the values' layout) of a head; D/8 lanes take eight channels
 // each and go through the octet's tokens, all of whose loads are under way before the first is used.  So a value's codes leave as
 // 32 contiguous bytes per lane where the whole octet is new, and no lane ever reads what another one writes.
-// 8 prompts of up to 8 192 tokens (8 heads of 128 channels, bf16, 254 MB read and written): 70 us, 3.6 TB/s, waiting for memory; 16 trees of 60 nodes 7 us.
+// 8 prompts of up to 8 192 tokens (8 heads of 128 channels, bf16, 254 MB read and written): 65 us, 3.9 TB/s, waiting for memory; 16 trees of 60 nodes 6.5 us.
 template <int D, typename T>
 __global__ void __launch_bounds__(256) append_kernel(Cache c, size_t layer_offset, const int32_t* __restrict__ seqs, Rows<const T> k,
                                                      Rows<const T> v, const int32_t* __restrict__ n_new, int B, int N, int octets,
@@ -51,12 +51,12 @@ __global__ void __launch_bounds__(256) append_kernel(Cache c, size_t layer_offse
   // the octet's tokens among the new ones: positions start + from .. start + to - 1
   const int from = max(len - start, 0), to = page < 0 ? 0 : min(len + n - start, 8);
 
-  Eight kx[8], vx[8];
+  Raw<T> kr[8], vr[8];  // (widened one by one: twice the registers otherwise, and three waves per SIMD instead of five with bf16)
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     if (j >= from && j < to) {
-      kx[j] = load_eight(k.at(b, start + j - len, h) + lane * 8);
-      vx[j] = load_eight(v.at(b, start + j - len, h) + lane * 8);
+      kr[j] = load_raw(k.at(b, start + j - len, h) + lane * 8);
+      vr[j] = load_raw(v.at(b, start + j - len, h) + lane * 8);
     }
   }
   const u32 t0 = start & ((1 << c.log_page) - 1);
@@ -67,14 +67,15 @@ __global__ void __launch_bounds__(256) append_kernel(Cache c, size_t layer_offse
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const bool here = j >= from && j < to;
-    const u32 kt = here ? top_bits(kx[j]) : 0, vt = here ? top_bits(vx[j]) : 0;
+    const Eight kx = widen(kr[j]), vx = widen(vr[j]);
+    const u32 kt = here ? top_bits(kx) : 0, vt = here ? top_bits(vx) : 0;
     const bool bad = (__ballot(max(kt, vt) >= 0x7F800000u) & mine) != 0;
     const u32 kb = scale_byte(block_top(kt)), vb = scale_byte(block_top(vt));
     vw[j] = vs[j] = 0;
     if (here) {
-      *reinterpret_cast<u32*>(base + Place<D>::key(t0 + j) + lane * 4) = bad ? 0 : encode(kx[j], kb);
+      *reinterpret_cast<u32*>(base + Place<D>::key(t0 + j) + lane * 4) = bad ? 0 : encode(kx, kb);
       if (lane % 4 == 0) base[Place<D>::key_scale(c.log_page, t0 + j) + lane / 4] = static_cast<uint8_t>(bad ? kNanScale : kb);
-      vw[j] = bad ? 0 : encode(vx[j], vb);
+      vw[j] = bad ? 0 : encode(vx, vb);
       vs[j] = bad ? kLeastScale : vb;
     }
   }
