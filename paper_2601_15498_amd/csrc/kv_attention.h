@@ -6,7 +6,7 @@
 // formed in.  A conversion of codes to bf16 is exact; it gives two channels of one key where the second product takes two keys of one channel: a
 // byte permutation per two values.
 //
-// Few rows (Narrow, up to 32): the four waves of a work-group take every fourth tile of the same rows and meet in LDS at the end.  Bound by the cache's way from
+// Few rows (Narrow, 16 or 32 at a time): the four waves of a work-group take every fourth tile of the same rows and meet in LDS at the end.  Bound by the cache's way from
 // memory: 64 tokens over 500 - 8 192, 304 MB, 73 us, of which in the middle 8.5 TB/s, the rest is the beginning and the end.
 // More (Wide): each of four or eight waves has 32 rows of its own, the values are converted once for all of them.  Bound by the matrix cores and the vector
 // instructions between them, and by the clock that the card keeps meanwhile.
