@@ -58,8 +58,9 @@ template <typename F> static int by_type(int dtype, F f) { return dtype == MARS_
 
 static int row_octets(int N) { return (N + 6) / 8 + 1; }  // octets that N positions can touch
 
-// Work-groups of a commit: 256 paths in 32 layers and 8 heads take 40 us by about 2 048, 47 by 512, 69 by 16 384.
-constexpr int kCommitGroups = 2048;
+// Work-groups of a commit, as long as each has as many layers as it takes at a time: 256 paths in 32 layers and 8 heads 45 us by about 4 096, 50 by
+// 2 048; 32 paths 9.5 us by 512 of two layers, 11 by 1 024 of one.
+constexpr int kCommitGroups = 4096;
 // Pools of up to this many pages are searched for free ones by 256 threads (four steps): one request's two children 16.8 us, by 1 024 threads 18.5;
 // in a pool of 60 000 pages 107 and 103.
 constexpr int kPlanFewPages = 16384;
@@ -251,10 +252,10 @@ int mars_kv_commit(const mars_kv_cache* cache, const int32_t* seqs, const int32_
                    int32_t* new_lens, int32_t* status, void* hip_stream) {
   Cache c;
   if (!batch_ok(B, N) || !cache_ok(cache, POOL | TABLE | LENS, &c) || !accept_len || !path_idx || !new_lens) return MARS_ERR_ARG;
-  // layers per work-group: so that the chip holds about all of them at once
+  // layers per work-group
   const long quads = static_cast<long>(B) * ((c.heads + 3) / 4);
-  const int per_group = static_cast<int>((quads * c.layers + kCommitGroups - 1) / kCommitGroups);
-  const int layers = per_group < c.layers ? per_group : c.layers;
+  const long even = (quads * c.layers + kCommitGroups - 1) / kCommitGroups, per_group = even < kCommitDeep ? kCommitDeep : even;
+  const int layers = per_group < c.layers ? static_cast<int>(per_group) : c.layers;
   const long groups = quads * ((c.layers + layers - 1) / layers);
   if (groups > 0x7FFFFFFFl) return MARS_ERR_ARG;
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);

@@ -199,13 +199,15 @@ template <int D> __device__ __forceinline__ u32 scale_byte_at(u32 log_page, u32 
   return i < D / 32 ? Place<D>::key_scale(log_page, t) + i : Place<D>::value_scale(log_page, t) + (i - D / 32) * 8;
 }
 // The path is looked at once for `per_group` layers: a wave's chain of loads (length, path, pages) costs as much as a dozen rows, and with a work-group per layer
-// 256 paths in 32 layers took 8 rounds of it (67 us; now 40 to 48, some 160 MB in pieces of four bytes of the values and 64 of the keys, a third of which have
-// to move).  16 paths in 32 layers: 7 us, latency.
+// 256 paths in 32 layers took 8 rounds of it (67 us; now 45 from memory and 35 from the memory-side cache, some 160 MB in pieces of four bytes of the values and
+// 64 of the keys, a third of which have to move).  16 paths in 32 layers: 7 us, latency.  Two layers at a time: with four, the registers leave room for four waves
+// per SIMD (64 paths 16 us instead of 13.5, of 256 channels 24 instead of 14).
+constexpr int kCommitDeep = 2;
 template <int D>
 __global__ void __launch_bounds__(256) commit_kernel(Cache c, const int32_t* __restrict__ seqs, const int32_t* __restrict__ accept_len,
                                                      const int32_t* __restrict__ path_idx, int B, int N, int per_group,
                                                      int32_t* __restrict__ new_lens, int32_t* __restrict__ status) {
-  constexpr int BATCH = 8, DEEP = 4;               // rows, and layers of them, on their way at a time
+  constexpr int BATCH = 8, DEEP = kCommitDeep;     // rows, and layers of them, on their way at a time
   constexpr int WORDS = D / 4, BYTES = D / 16;     // of a row
   constexpr int WORD_OPS = BATCH * WORDS / kWave, BYTE_OPS = (BATCH * BYTES + kWave - 1) / kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
