@@ -78,7 +78,7 @@ struct AttnPlan {
 // caches of 1 024 - 8 191: 175 and 169; 100 rows: 89 and 77).
 // In 32 bits the products take three times as long and 32 rows a third more registers: up to 80 rows 16 at a time are faster (48 rows: 47 us instead of 71, 80
 // rows: 66 and 77; 120 rows: 97 and 84).
-static AttnPlan attn_plan(int N, int group, int dim, int dtype) {
+static AttnPlan attn_plan(int N, int group, int dim, int dtype, int page) {
   const long rows = static_cast<long>(N) * group;
   const bool f32 = dtype == MARS_F32;
   AttnPlan p;
@@ -86,7 +86,7 @@ static AttnPlan attn_plan(int N, int group, int dim, int dtype) {
   p.rows = p.mode == KEYS && (f32 || rows <= 16) ? 16 : 32;
   const long four = (rows + kWaves * 32 - 1) / (kWaves * 32);  // blocks of four waves
   p.waves = p.mode == ROWS && four % 2 == 0 && !f32 && dim <= 128 ? 2 * kWaves : kWaves;
-  p.groups = 256 * per_unit(dim, p.mode, p.waves, p.rows, f32);
+  p.groups = 256 * per_unit(dim, p.mode, p.waves, p.rows, f32, page >= kTile);
   p.nodes = (p.mode == ROWS ? p.waves * p.rows : p.rows) / group;
   // (a wave's piece: its rows' references and sums, and its results)
   const size_t piece = sizeof(float) * (2 * p.rows + static_cast<size_t>(p.rows) * dim);
@@ -97,10 +97,10 @@ static AttnPlan attn_plan(int N, int group, int dim, int dtype) {
 // heads, 1 021 tokens: 12 us, cut 15; 1 500: 15 and 12.5.  Where there are blocks enough for half the compute units, and each is a few rows of bf16
 // (light), cutting wins less: 32 times one token over 1 900 - 2 000, 256 blocks: 19 us, cut 28; 8 times, 64 blocks: 18.6 and 17.7.
 static int whole_units(bool light, long blocks) { return light && blocks >= 128 ? 16 : 8; }
-// The same where the lengths decide (the second kernel runs in any case then), in units beyond an even share: 64 times one token over 500 - 2 000 26 us with
-// 12, 32 with 8; one over 1 500 18 and 13.  With more rows a unit takes longer: 8 trees of 240 rows over 1 000 - 1 900 72 us with 12, 46 with 8, 46 with 0; 32 such
-// trees 80, 80 and 94.
-static u32 join_cost(bool light, long blocks) { return light && blocks >= 128 ? 12 : 8; }
+// The same where the lengths decide (the second kernel runs in any case then), in units beyond an even share: 64 times one token over 5 000 67 us with 20, 82 with
+// 12, 128 over 500 - 4 000 69 and 82; one over 1 500 18 and 13.  With more rows a unit takes longer: 8 trees of 240 rows over 1 000 - 1 900 72 us with 12, 46
+// with 8, 46 with 0; 32 such trees 80, 80 and 94.
+static u32 join_cost(bool light, long blocks) { return light && blocks >= 128 ? 20 : 8; }
 
 // Units that a work-group takes at least: with two, pieces are half as many to join.  One token over 4 000: 14.7 us instead of 17.9, 8 over 1 500
 // 14.9 and 19.0, 2 trees of 240 rows over 1 900 36 and 41; but 2 of 28 rows over 1 000 - 1 900 23.6 and 19.0, 2 of 7 in fp32 16.4 and 14.6, whose
@@ -195,7 +195,7 @@ static bool attention_sizes_ok(int B, int N, int q_heads, int heads, int dim) {
 
 size_t mars_kv_attention_workspace_bytes(int B, int N, int q_heads, int heads, int dim, int dtype) {
   if (!attention_sizes_ok(B, N, q_heads, heads, dim) || !dtype_ok(dtype)) return 0;
-  return attn_plan(N, q_heads / heads, dim, dtype).bytes;
+  return attn_plan(N, q_heads / heads, dim, dtype, kTile).bytes;  // (for pages of less it may be more than is wanted)
 }
 
 int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs, const mars_kv_rows* q, int dtype, int q_heads,
@@ -208,7 +208,7 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
   if (!dtype_ok(dtype)) return MARS_ERR_DTYPE;
   if (!rows_ok(q, dtype) || !rows_ok(out, dtype) || max_len < 0 || !(scale > 0.0f) || !std::isfinite(scale) || (mask && N > MARS_MAX_NODES))
     return MARS_ERR_ARG;
-  const AttnPlan p = attn_plan(N, q_heads / c.heads, cache->dim, dtype);
+  const AttnPlan p = attn_plan(N, q_heads / c.heads, cache->dim, dtype, cache->page);
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < p.bytes) return MARS_ERR_WORKSPACE;
   AttnArgs a{};
   a.c = c;

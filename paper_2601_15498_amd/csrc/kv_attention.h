@@ -7,7 +7,7 @@
 // byte permutation per two values.
 //
 // Few rows (Narrow, 16 or 32 at a time): the four waves of a work-group take every fourth tile of the same rows and meet in LDS at the end.  Bound by the cache's way from
-// memory: 64 tokens over 500 - 8 192, 304 MB, 73 us, of which in the middle 8.5 TB/s, the rest is the beginning and the end.
+// memory: 64 tokens over 500 - 8 192, 304 MB, 69 us, of which in the middle 8.5 TB/s, the rest is the beginning and the end.
 // More (Wide): each of four or eight waves has 32 rows of its own, the values are converted once for all of them.  Bound by the matrix cores and the vector
 // instructions between them, and by the clock that the card keeps meanwhile.
 // The work is dealt out by kv_deal.h: a work-group takes a run of tiles that may begin and end inside a block of rows; what it has of such a
@@ -686,20 +686,23 @@ template <typename T, int D> __device__ __forceinline__ void clear_rows(const At
 }
 
 // Work-groups that have to fit a compute unit beside each other: what the compiler may give a wave of registers, and the ring of LDS.
-constexpr int per_unit(int D, int mode, int waves, int rows, bool f32) {
-  if (mode == KEYS) return (D == 256 ? 1 : 2) + (rows == 16 && !f32 ? 1 : 0);
+// 16 rows of bf16 fit the 128 registers of four waves per SIMD where a tile lies in one page (uniform): 64 tokens over 500 - 8 192 67 us, three 72; where it does not,
+// pages of 16 tokens 99 and 73.
+constexpr int per_unit(int D, int mode, int waves, int rows, bool f32, bool uniform) {
+  if (mode == KEYS) return (D == 256 ? 1 : 2) + (rows == 16 && !f32 ? (D <= 128 && uniform ? 2 : 1) : 0);
   return D == 256 || waves > kWaves ? 1 : 2;
 }
-template <typename W> constexpr int kPerUnit = per_unit(W::D, W::MODE, W::kGroupWaves, W::kRows, std::is_same<typename W::T, float>::value);
+template <typename W, bool UNIFORM>
+constexpr int kPerUnit = per_unit(W::D, W::MODE, W::kGroupWaves, W::kRows, std::is_same<typename W::T, float>::value, UNIFORM);
 template <typename W> constexpr int kValuesBytes = W::MODE == ROWS ? W::kGroupWaves * W::D * 64 : 16;  // of two steps' values as operands
-template <typename W> constexpr int stages_of() {  // units in the ring, those that are worked on among them
-  constexpr int n = (160 * 1024 / kPerUnit<W> - 1024 - kValuesBytes<W>) / (kWaves * Tile<W::D>::kBytes);
+template <typename W, bool UNIFORM> constexpr int stages_of() {  // units in the ring, those that are worked on among them
+  constexpr int n = (160 * 1024 / kPerUnit<W, UNIFORM> - 1024 - kValuesBytes<W>) / (kWaves * Tile<W::D>::kBytes);
   return n > 4 ? 4 : n;
 }
 
 template <typename W, bool UNIFORM>
-__global__ void __launch_bounds__(W::kGroupWaves * kWave, kPerUnit<W> * W::kGroupWaves / kWaves) attention_kernel(AttnArgs a) {
-  constexpr int D = W::D, MODE = W::MODE, GROUP = W::kGroupWaves, STAGES = stages_of<W>();
+__global__ void __launch_bounds__(W::kGroupWaves * kWave, (kPerUnit<W, UNIFORM> * W::kGroupWaves / kWaves)) attention_kernel(AttnArgs a) {
+  constexpr int D = W::D, MODE = W::MODE, GROUP = W::kGroupWaves, STAGES = stages_of<W, UNIFORM>();
   // Units in flight behind the one that is waited for (in mode ROWS a step is half a unit, or a whole one by eight waves):
   constexpr int AHEAD = GROUP > kWaves ? STAGES - 3 : STAGES - 2;
   using X = Tile<D>;
