@@ -133,8 +133,8 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
  * lens[s] + 1 + i, behind the root's; new_lens[s] = lens[s] + 1 + accept_len[b].
  *   accept_len, path_idx   [B], [B][N] as mars_verify writes them.
  *   new_lens   out, [sequences]; only the sequences of the call are written.  May be lens itself.
- *   status     out, optional, [B]: MARS_KV_OK, MARS_KV_BAD_SEQUENCE, MARS_KV_BAD_PATH or MARS_KV_NO_PAGES (a row's page is
- *              missing).  With one of the last two nothing is moved and new_lens[s] = lens[s].
+ *   status     out, optional, [B]: MARS_KV_OK, MARS_KV_BAD_SEQUENCE, MARS_KV_BAD_PATH or MARS_KV_NO_PAGES (a row's page, or the
+ *              root's, is missing).  With one of the last two nothing is moved and new_lens[s] = lens[s].
  * The pages behind the new length stay with the sequence (the next step's nodes go there).  Reads page_table, lens.
  */
 int mars_kv_commit(const mars_kv_cache* cache, const int32_t* seqs, const int32_t* accept_len, const int32_t* path_idx, int B, int N,

@@ -175,14 +175,14 @@ __device__ __forceinline__ Path check_path(const Cache& c, const int32_t* seqs, 
   p.len = p.seq >= 0 ? c.lens[p.seq] : 0;
   p.n = accept_len[b];
   p.status = MARS_KV_OK;
-  bool bad = p.n < 0 || p.n >= N, missing = p.len < 0;
+  bool bad = p.n < 0 || p.n >= N, missing = p.seq >= 0 && page_of(c, p.seq, p.len) < 0;  // (the root's row; len < 0 has no page either)
   if (p.seq >= 0 && !bad) {
     const int32_t* path = path_idx + static_cast<size_t>(b) * N;
     for (int i = threadIdx.x % kWave; i < p.n; i += kWave) {
       const int node = path[i], before = i ? path[i - 1] : 0;
       const bool in = node > before && node < N;
       bad |= !in;
-      if (in && !missing) missing |= page_of(c, p.seq, p.len + node) < 0 || page_of(c, p.seq, p.len + 1 + i) < 0;
+      if (in) missing |= page_of(c, p.seq, p.len + node) < 0 || page_of(c, p.seq, p.len + 1 + i) < 0;
     }
   }
   if (p.seq < 0) p.status = MARS_KV_BAD_SEQUENCE;
