@@ -120,7 +120,7 @@ int mars_tree_mask(const int32_t* tree_parent, const int32_t* n_new, int B, int 
  * Scores, softmax statistics and sums are held in fp32.  For bf16 rows the probabilities are rounded to bf16 in front of the
  * product with the values (a relative error of at most 2^-8 per key, independent from key to key); for fp32 rows they and the queries go through the
  * matrix cores as three bf16 terms each.  Results are reproducible bit for bit.
- * A sequence number outside the cache gives rows of zeros; a page number outside it among a row's keys gives NaN.
+ * A sequence number outside the cache gives rows of zeros (without seqs: requests from `sequences` on); a page number outside it among a row's keys gives NaN.
  * Reads page_table, lens.
  */
 size_t mars_kv_attention_workspace_bytes(int B, int N, int q_heads, int heads, int dim, int dtype);

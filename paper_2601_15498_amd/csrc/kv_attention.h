@@ -715,7 +715,7 @@ __global__ void __launch_bounds__(W::kGroupWaves * kWave, (kPerUnit<W, UNIFORM> 
   __shared__ float sh_m[MODE == KEYS ? kWaves * W::kRows : 1], sh_l[MODE == KEYS ? kWaves * W::kRows : 1];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
 
-  if (a.n_new || a.seqs)  // (otherwise every request has N nodes)
+  if (a.n_new || a.seqs || a.B > a.c.sequences)  // (otherwise every request has N nodes)
     for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
       const int n = Request(a, b).n;
       if (n < a.N) clear_rows<typename W::T, D>(a, b, n);
