@@ -16,14 +16,16 @@ struct ReserveSpace {
   int32_t* copies;               // [1]
 };
 constexpr int kCopyBit = 1 << 30;  // of the pages a request wants: the first is to be a copy of the one it shares
-// Sum of v over the threads in front of this one, and over all.
+// Sums stop here: a call may want more pages than 32 bits count (more than there are in any case), and one request at most 2^27.
+__device__ __forceinline__ int plus(int a, int b) { return static_cast<int>(min(static_cast<u32>(a) + static_cast<u32>(b), 0x7FFFFFFFu)); }
+// Sum of v (>= 0) over the threads in front of this one, and over all.  Where it stops, it is no less than the last sum minus v.
 template <int THREADS> __device__ __forceinline__ int scan(int v, int* sh, int& total) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   int x = v;
 #pragma unroll
   for (int d = 1; d < kWave; d <<= 1) {
     const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
+    if (lane >= d) x = plus(x, y);
   }
   __syncthreads();  // (sh may still be read from the scan before)
   if (lane == kWave - 1) sh[wave] = x;
@@ -32,10 +34,10 @@ template <int THREADS> __device__ __forceinline__ int scan(int v, int* sh, int& 
   total = 0;
 #pragma unroll
   for (int w = 0; w < THREADS / kWave; ++w) {
-    if (w < wave) front += sh[w];
-    total += sh[w];
+    if (w < wave) front = plus(front, sh[w]);
+    total = plus(total, sh[w]);
   }
-  return front + x - v;
+  return plus(front, x) - v;
 }
 
 // One work-group: requests' wants, the lowest free pages, the tables.  What it knows of the requests lies in LDS.
@@ -100,7 +102,7 @@ __global__ void __launch_bounds__(THREADS) reserve_kernel(Cache c, const int32_t
     const int b = b0 + tid;
     int total;
     const int before = scan<THREADS>(b < B ? sh_wants[b] & ~kCopyBit : 0, sh, total);
-    if (b < B) sh_begin[b] = static_cast<int>(min(demand + before, 0x3FFFFFFFl));
+    if (b < B) sh_begin[b] = static_cast<int>(min(demand + before, 0x7FFFFFFFl));
     demand += total;
   }
 
@@ -138,7 +140,7 @@ __global__ void __launch_bounds__(THREADS) reserve_kernel(Cache c, const int32_t
   for (int b0 = 0; b0 < B; b0 += THREADS) {
     const int b = b0 + tid;
     const int want = b < B ? sh_wants[b] & ~kCopyBit : 0;
-    const bool fits = b < B && sh_begin[b] + want <= have, copy = fits && (sh_wants[b] & kCopyBit);
+    const bool fits = b < B && static_cast<long>(sh_begin[b]) + want <= have, copy = fits && (sh_wants[b] & kCopyBit);
     int total;
     const int rank = copies + scan<THREADS>(copy, sh, total);
     copies += total;
