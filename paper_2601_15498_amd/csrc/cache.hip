@@ -107,6 +107,15 @@ static u32 join_cost(bool light, long blocks) { return light && blocks >= 128 ? 
 // units take longer and whose pieces are small.  (Three: one token over 2 000 15.2 instead of 12.2.)
 static u32 least_share(const AttnPlan& p, int dtype) { return p.mode == KEYS && (dtype == MARS_F32 || p.rows == 32) ? 1 : 2; }
 
+// The most that a call deals out, as kv_deal.h counts it (in 32 bits): units of blocks or of pairs of blocks -- of an odd number, the last pair is as
+// large as the others -- or two per item.
+static double most_dealt(int B, int N, int heads, int nodes, bool masked, long most_len) {
+  const long blocks = (static_cast<long>(N) + nodes - 1) / nodes;
+  const bool paired = !masked && blocks > 1;
+  const long per = paired ? (2 * most_len + (blocks + 1) * nodes + 2 * (kUnit - 1)) / kUnit : (most_len + N + kUnit - 1) / kUnit;
+  return static_cast<double>(B) * heads * (paired ? (blocks + 1) / 2 : blocks) * (per > 2 ? per : 2);
+}
+
 template <typename W> static int launch_attention(u32 groups, const AttnArgs& a, hipStream_t stream) {
   static_assert(Piece<W>::kFloats == 2 * W::kRows + W::kRows * W::D, "as attn_plan counts them");
   if (a.c.log_page >= 5) hipLaunchKernelGGL((attention_kernel<W, true>), dim3(groups), dim3(W::kGroupWaves * kWave), 0, stream, a);
@@ -209,6 +218,8 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
   if (!rows_ok(q, dtype) || !rows_ok(out, dtype) || max_len < 0 || !(scale > 0.0f) || !std::isfinite(scale) || (mask && N > MARS_MAX_NODES))
     return MARS_ERR_ARG;
   const AttnPlan p = attn_plan(N, q_heads / c.heads, cache->dim, dtype, cache->page);
+  const long most_len = static_cast<long>(c.width) << c.log_page;
+  if (most_dealt(B, N, c.heads, p.nodes, mask != nullptr, most_len) > 4.0e9) return MARS_ERR_ARG;
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < p.bytes) return MARS_ERR_WORKSPACE;
   AttnArgs a{};
   a.c = c;
@@ -225,9 +236,8 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
   a.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
   a.B = B; a.N = N; a.q_heads = q_heads; a.group = q_heads / c.heads; a.words = (N + 63) / 64;
   a.nodes = p.nodes;
-  const long most_len = static_cast<long>(c.width) << c.log_page, blocks = static_cast<long>(B) * c.heads * ((N + p.nodes - 1) / p.nodes);
-  const double units = static_cast<double>(blocks) * ((most_len + N + 3 * kUnit) / kUnit);  // at most; counted in 32 bits
-  if (units > 4.0e9) return MARS_ERR_ARG;
+  const long blocks = static_cast<long>(B) * c.heads * ((N + p.nodes - 1) / p.nodes);
+  const double units = static_cast<double>(blocks) * ((most_len + N + 3 * kUnit) / kUnit);  // at most, about
   const bool light = p.mode == KEYS && dtype == MARS_BF16;
   a.whole = ((max_len && max_len < most_len ? max_len : most_len) + N + kUnit - 1) / kUnit <= whole_units(light, blocks);
   a.join_cost = join_cost(light, blocks);
