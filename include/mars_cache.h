@@ -22,7 +22,8 @@
  *   keys' scales   [page][dim/32]
  *   values' scales [page/8][dim/32][8]
  *
- * The tables.  page_table [sequences][width]: the pages of a sequence, then -1.  lens [sequences]: committed tokens.
+ * The tables.  page_table [sequences][width]: the pages of a sequence, then -1.  lens [sequences]: committed tokens; the caller may lower it
+ * between calls (the sequence goes on from an earlier token; its pages stay).
  * held [sequences]: pages in the table's row.  refs [pages]: how many sequences hold a page; a page is free exactly when that is
  * 0, there is no other list, and free pages are given out lowest first.  An empty cache is page_table = -1 and zeros in the other three.
  *
@@ -141,12 +142,13 @@ int mars_kv_commit(const mars_kv_cache* cache, const int32_t* seqs, const int32_
                    int32_t* new_lens, int32_t* status, void* hip_stream);
 
 /*
- * Room for n_new[b] (NULL: N) tokens behind lens[s]: pages are added to the sequence's row, and where the first of these tokens goes into a page that
- * others hold too, the sequence gets a copy of it in all layers (in its place in the row).  Where all holders of a page
- * ask for room in one call, the last of them keeps the page.  Free pages are given out lowest first, request by request.
+ * Room for n_new[b] (NULL: N) tokens behind lens[s], in pages that are the sequence's own: pages are added to its row, and a page in the row that these
+ * tokens go into and that others hold too is replaced by a free one -- the first of them, if committed tokens are in it, by a copy in all
+ * layers.  Where all holders of a page write it in one call, the last of them keeps the page.  Free pages are given out lowest first, request by
+ * request: in place of shared ones in the order of the row, then the added ones.
  *   status     out, optional, [B]: MARS_KV_OK, MARS_KV_BAD_SEQUENCE, MARS_KV_TOO_LONG, or MARS_KV_NO_PAGES; other than OK:
  *              nothing was changed for this request.  When the pages run out, every later request that needs one goes without, and so
- *              does the last holder of a page of which an earlier one did not get its copy.
+ *              does the last holder of a page of which an earlier one did not get its own.
  *   workspace  256-byte aligned, >= mars_kv_reserve_workspace_bytes(pages, B).
  * Sequences of a call differ from each other.  Reads and writes all tables.
  */

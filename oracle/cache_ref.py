@@ -134,12 +134,16 @@ class Tables:
         self.lens, self.held = np.zeros(sequences, np.int32), np.zeros(sequences, np.int32)
         self.refs = np.zeros(pages, np.int32)
 
+    def written(self, s, m):
+        """Places in its row of the pages held by s that m new tokens go into."""
+        return range(self.lens[s] // self.P, min(self.held[s], -(-(self.lens[s] + m) // self.P))) if m > 0 else range(0)
+
     def reserve(self, seqs, n):
         status, copied = [], []
-        wants, shared = [], []
-        for s, m in zip(seqs, n):
+        wants, into, asks = [], [], {}
+        for i, (s, m) in enumerate(zip(seqs, n)):
             status.append(self.OK)
-            shared.append(-1)
+            into.append(range(0))
             wants.append(0)
             if not 0 <= s < len(self.lens):
                 status[-1] = self.BAD_SEQUENCE
@@ -149,17 +153,17 @@ class Tables:
                 status[-1] = self.TOO_LONG
                 continue
             wants[-1] = max(0, need - self.held[s])
-            at = self.lens[s] // self.P
-            if self.lens[s] % self.P and m > 0 and at < self.held[s]:
-                shared[-1] = self.table[s, at]
-        copy = []
-        for i, page in enumerate(shared):
-            holders = self.refs[page] if page >= 0 else 0
-            copy.append(holders > 1 and (page in shared[i + 1:] or holders > shared.count(page)))
+            into[-1] = self.written(s, m)
+            for j in into[-1]:
+                asks.setdefault(int(self.table[s, j]), []).append(i)
+        # a page that others hold too is given up, but not by the last of its holders where all of them are here
+        given = [[j for j in js if self.refs[self.table[seqs[i], j]] > 1
+                  and (asks[self.table[seqs[i], j]][-1] != i or len(asks[self.table[seqs[i], j]]) < self.refs[self.table[seqs[i], j]])]
+                 for i, js in enumerate(into)]
         free = [p for p in range(len(self.refs)) if self.refs[p] == 0]
         out = False
         for i, s in enumerate(seqs):
-            k = wants[i] + copy[i]
+            k = wants[i] + len(given[i])
             if k == 0:
                 continue
             out |= k > len(free)
@@ -168,16 +172,16 @@ class Tables:
                 continue
             got, free = free[:k], free[k:]
             self.refs[got] = 1
-            if copy[i]:
-                self.refs[shared[i]] -= 1
-                self.table[s, self.lens[s] // self.P] = got[0]
-                copied.append((shared[i], got[0]))
-                got = got[1:]
-            for page in got:
+            for j, page in zip(given[i], got):
+                old, self.table[s, j] = self.table[s, j], page
+                self.refs[old] -= 1
+                if j * self.P < self.lens[s]:        # committed tokens are in it
+                    copied.append((old, page))
+            for page in got[len(given[i]):]:
                 self.table[s, self.held[s]] = page
                 self.held[s] += 1
-        for i, page in enumerate(shared):            # the last holder, where an earlier one went without its copy
-            if page >= 0 and not copy[i] and status[i] == self.OK and self.refs[page] > 1:
+        for i, js in enumerate(into):                # the last holder, where an earlier one went without a page of its own
+            if status[i] == self.OK and any(self.refs[self.table[seqs[i], j]] > 1 for j in js):
                 status[i] = self.NO_PAGES
         return status, copied
 

@@ -258,8 +258,8 @@ def alloc_reserve_workspace(pool: torch.Tensor, B: int) -> torch.Tensor:
 
 def mars_kv_reserve(pool: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, held: torch.Tensor, refs: torch.Tensor, n, *,
                     page_size: int, seqs: torch.Tensor = None, status: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
-    """Room for n tokens (an int for all requests, or [B] int32) behind the committed ones; pages that others hold too are copied where they
-    would be written.  Returns the status of every request."""
+    """Room for n tokens (an int for all requests, or [B] int32) behind the committed ones; pages that others hold too are replaced where
+    they would be written, by copies as far as committed tokens are in them.  Returns the status of every request."""
     rc = (_native or _calls()).reserve(pool, page_table, lens, held, refs, n, page_size, seqs, status, workspace, _stream)
     if rc is not None:
         _check(rc)

@@ -126,13 +126,16 @@ template <typename W> static int launch_attention(u32 groups, const AttnArgs& a,
   return launched();
 }
 
-static ReserveSpace reserve_space(char* ws, int B) {
-  const size_t n = align_up(sizeof(int32_t) * B);
+static ReserveSpace reserve_space(char* ws, int pages, int B) {
+  const size_t n = align_up(sizeof(int32_t) * B), all = align_up(sizeof(int32_t) * pages);
   ReserveSpace r;
   r.copy_src = reinterpret_cast<int32_t*>(ws);
   r.copy_dst = reinterpret_cast<int32_t*>(ws + n);
   r.copies = reinterpret_cast<int32_t*>(ws + 2 * n);
   r.found = reinterpret_cast<int32_t*>(ws + 2 * n + kAlign);
+  r.former = reinterpret_cast<int32_t*>(ws + 2 * n + kAlign + all);
+  r.asks = reinterpret_cast<int32_t*>(ws + 2 * n + kAlign + 2 * all);
+  r.last = reinterpret_cast<int32_t*>(ws + 2 * n + kAlign + 3 * all);
   return r;
 }
 static u32 copy_groups(const Cache& c, long pairs) {
@@ -282,7 +285,7 @@ int mars_kv_commit(const mars_kv_cache* cache, const int32_t* seqs, const int32_
 
 size_t mars_kv_reserve_workspace_bytes(int pages, int B) {
   if (pages < 1 || pages > (1 << 30) || B < 1 || B > MARS_KV_MAX_REQUESTS) return 0;
-  return 2 * align_up(sizeof(int32_t) * B) + kAlign + align_up(sizeof(int32_t) * pages);
+  return 2 * align_up(sizeof(int32_t) * B) + kAlign + 4 * align_up(sizeof(int32_t) * pages);
 }
 
 int mars_kv_reserve(const mars_kv_cache* cache, const int32_t* seqs, const int32_t* n_new, int B, int N, int32_t* status, void* workspace,
@@ -291,7 +294,7 @@ int mars_kv_reserve(const mars_kv_cache* cache, const int32_t* seqs, const int32
   if (!batch_ok(B, N) || !cache_ok(cache, POOL | TABLE | LENS | HELD | REFS, &c)) return MARS_ERR_ARG;
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < mars_kv_reserve_workspace_bytes(c.pages, B))
     return MARS_ERR_WORKSPACE;
-  const ReserveSpace ws = reserve_space(static_cast<char*>(workspace), B);
+  const ReserveSpace ws = reserve_space(static_cast<char*>(workspace), c.pages, B);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (B <= kPlanFew && c.pages <= kPlanFewPages)
     hipLaunchKernelGGL(reserve_kernel<kPlanFew>, dim3(1), dim3(kPlanFew), 0, stream, c, seqs, n_new, B, N, status, ws);
