@@ -24,8 +24,12 @@
 namespace mars {
 namespace kv {
 
-constexpr float kFloor = -3.0e38f;    // the reference before the first key that counts
-constexpr float kSlack = 8.0f;        // how far (in powers of two) scores may pass the reference before it is moved up
+constexpr float kFloor = -3.402823466e38f;  // the reference before the first key that counts: the least number, so that all scores pass it
+constexpr float kSlack = 8.0f;              // how far (in powers of two) scores may pass the reference before it is moved up
+// exp2(c s - m) is formed without rounding c s, so that the key that m is of gives 2 to what m was rounded by.  Beyond this (2^24) that is half a power of two and
+// more, at 2^31 all of the exponent's range: there c s is rounded first, as m was, and the largest scores are the reference exactly.
+constexpr float kLarge = 16777216.0f;
+__device__ __forceinline__ bool any_large(float m) { return __any(__builtin_fabsf(m) > kLarge && m != kFloor); }
 enum { KEYS = 0, ROWS = 1 };          // what the waves of a work-group divide between them
 
 // (Written out: fmaxf would first quiet each operand.  The compiler does not wait for a matrix instruction's results in front of it: `a` comes from an
@@ -259,12 +263,14 @@ template <int D_, int RB, typename T_> struct Narrow {
   Queries16<D, RB, T> q;
   f32x4 o[RB][NF];                              // [f][i]: channel (4g + i) D/16 + f
   float m[RB], l[RB];
+  bool large;                                   // (the same for the wave) a reference beyond kLarge
   int node[RB];                                 // of this lane's rows; < 0: no row
   unsigned long long word[RB];                  // the row's mask, where it is one word
 
   // Rows row0 .. of the block of nodes from node0 on, which has `rows`.
   __device__ __forceinline__ void start(const AttnArgs& a, int b, int head, int node0, int row0, int rows) {
     const int r = threadIdx.x % 16;
+    large = false;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const RowOf<T> row(a, b, head, node0, row0 + rb * 16 + r, rows);
@@ -314,24 +320,27 @@ template <int D_, int RB, typename T_> struct Narrow {
       up |= top[rb] > m[rb] + kSlack;
     }
     if (__any(up)) {  // seldom after the first tiles
+      large = false;
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         float t = fmaxf(top[rb], __shfl_xor(top[rb], 16));
         t = fmaxf(m[rb], fmaxf(t, __shfl_xor(t, 32)));
         const float shrink = __builtin_amdgcn_exp2f(m[rb] - t);
         m[rb] = t;
+        large |= any_large(t);
         l[rb] *= shrink;
 #pragma unroll
         for (int f = 0; f < NF; ++f) o[rb][f] *= shrink;
       }
     }
+    const float before = large ? c : 1.0f, factor = large ? 1.0f : c;  // (a branch instead would cost registers that four waves per SIMD do not have)
     u32 p[TERMS][RB][4];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
       for (int h = 0; h < 4; ++h) {
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[h / 2][rb][h % 2 * 2], c, -m[rb]));
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[h / 2][rb][h % 2 * 2 + 1], c, -m[rb]));
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[h / 2][rb][h % 2 * 2] * before, factor, -m[rb]));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[h / 2][rb][h % 2 * 2 + 1] * before, factor, -m[rb]));
         l[rb] += e0 + e1;
         u32 t[TERMS];
         split_pair<TERMS>(e0, e1, t);
@@ -556,6 +565,7 @@ template <int D_, typename T_, int WAVES> struct Wide {
   Keys32<D> next;                               // of the next tile
   f32x16 o[C];                                  // [block][i]: channel C (8 (i/4) + 4h + i%4) + block
   float m, l;
+  bool large;                                   // (the same for the wave) a reference beyond kLarge
   int node;                                     // of this lane's row; < 0: no row
   unsigned long long word;
 
@@ -566,6 +576,7 @@ template <int D_, typename T_, int WAVES> struct Wide {
     q.load(row.q, node >= 0);
     m = kFloor;
     l = 0.0f;
+    large = false;
 #pragma unroll
     for (int k = 0; k < C; ++k) o[k] = f32x16{};
   }
@@ -604,15 +615,21 @@ template <int D_, typename T_, int WAVES> struct Wide {
       top = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)));
       const float shrink = __builtin_amdgcn_exp2f(m - top);
       m = top;
+      large = any_large(m);
       l *= shrink;
 #pragma unroll
       for (int k = 0; k < C; ++k) o[k] *= shrink;
+    }
+    float factor = c;
+    if (large) {
+      s *= c;
+      factor = 1.0f;
     }
     next = Keys32<D>(after);  // (5% faster here than in front of the branches)
     u32 p[TERMS][2][4];  // probabilities, in terms, of the two steps of the product with the values
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * i], c, -m)), e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], c, -m));
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * i], factor, -m)), e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], factor, -m));
       l += e0 + e1;
       u32 x[TERMS];
       split_pair<TERMS>(e0, e1, x);
