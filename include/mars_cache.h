@@ -114,7 +114,7 @@ int mars_tree_mask(const int32_t* tree_parent, const int32_t* n_new, int B, int 
  *   n_new      [B], or NULL: N for all.  Rows from n_new[b] on see nothing, not even committed tokens.
  *   mask       [B][N][(N + 63)/64] uint64, bit j of row i: row i sees node j (any mask; mars_tree_mask makes a tree's); N <= MARS_MAX_NODES.
  *              NULL: a chain, row i sees nodes 0 .. i; any N.
- *   scale      > 0.
+ *   scale      > 0, and scale * log2(e) finite in fp32.
  *   max_len    HOST: what the lens are expected not to exceed; 0: the table's width times page.  It only guides how the work is split:
  *              longer sequences are attended in full.
  *   workspace  256-byte aligned, >= mars_kv_attention_workspace_bytes(...); scratch, calls that share it must not overlap.

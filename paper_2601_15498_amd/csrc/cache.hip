@@ -218,7 +218,8 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
       !attention_sizes_ok(B, N, q_heads, c.heads, cache->dim))
     return MARS_ERR_ARG;
   if (!dtype_ok(dtype)) return MARS_ERR_DTYPE;
-  if (!rows_ok(q, dtype) || !rows_ok(out, dtype) || max_len < 0 || !(scale > 0.0f) || !std::isfinite(scale) || (mask && N > MARS_MAX_NODES))
+  const float scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
+  if (!rows_ok(q, dtype) || !rows_ok(out, dtype) || max_len < 0 || !(scale > 0.0f) || !std::isfinite(scale_log2) || (mask && N > MARS_MAX_NODES))
     return MARS_ERR_ARG;
   const AttnPlan p = attn_plan(N, q_heads / c.heads, cache->dim, dtype, cache->page);
   const long most_len = static_cast<long>(c.width) << c.log_page;
@@ -236,7 +237,7 @@ int mars_kv_attention(const mars_kv_cache* cache, int layer, const int32_t* seqs
   a.out_request = out->request; a.out_node = out->node; a.out_head = out->head;
   a.lse = lse;
   a.partial = static_cast<float*>(workspace);
-  a.scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
+  a.scale_log2 = scale_log2;
   a.B = B; a.N = N; a.q_heads = q_heads; a.group = q_heads / c.heads; a.words = (N + 63) / 64;
   a.nodes = p.nodes;
   const long blocks = static_cast<long>(B) * c.heads * ((N + p.nodes - 1) / p.nodes);

@@ -35,3 +35,12 @@ def test_work_that_cannot_be_counted_is_refused(C, B, N, heads, mask, width, fit
     rows = C.RowsStruct(P, 1 << 20, 1 << 12, 64)
     rc = C.lib().mars_kv_attention(cache, 0, None, rows, 1, heads, None, P if mask else None, 1.0, 0, rows, None, B, N, 0x100000, 1, None)
     assert rc == (WORKSPACE if fits else ARG)
+
+
+@pytest.mark.parametrize("scale,ok", [(1e-45, True), (2.3e38, True), (2.4e38, False), (3.4e38, False)])
+def test_a_scale_whose_powers_of_two_are_no_number_is_refused(C, scale, ok):
+    """The kernels take exp2(scale * log2(e) * score): the factor has to be a number in 32 bits."""
+    rows = C.RowsStruct(P, 1 << 20, 1 << 12, 64)
+    rc = C.lib().mars_kv_attention(C.CacheStruct(P, P, P, P, P, 1, 4, 2, 64, 16, 3, 8), 0, None, rows, 1, 2, None, None, scale, 0, rows, None, 2, 3, 0x100000, 1,
+                                   None)
+    assert rc == (WORKSPACE if ok else ARG)
