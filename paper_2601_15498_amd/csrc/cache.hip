@@ -61,9 +61,10 @@ static int row_octets(int N) { return (N + 6) / 8 + 1; }  // octets that N posit
 // Work-groups of a commit, as long as each has as many layers as it takes at a time: 256 paths in 32 layers and 8 heads 45 us by about 4 096, 50 by
 // 2 048; 32 paths 9.5 us by 512 of two layers, 11 by 1 024 of one.
 constexpr int kCommitGroups = 4096;
-// Pools of up to this many pages are searched for free ones by 256 threads (four steps): one request's two children 16.8 us, by 1 024 threads 18.5;
-// in a pool of 60 000 pages 107 and 103.
-constexpr int kPlanFewPages = 16384;
+// Pools of up to this many pages are searched for free ones by 256 threads (two steps of 4 096), larger ones by 1 024: two requests of 60 tokens, the free pages the last
+// ones, 7.4 us by 256 threads and 7.6 by 1 024 in a pool of 4 000 pages, 8.0 and 7.1 in one of 16 000, 16 and 10 in one of 60 000 (106 and 55 us in one of 400 000: 128
+// requests).
+constexpr int kPlanFewPages = 8192;
 
 // ---------------------------------------------------------------- attention: how the work is laid out
 struct AttnPlan {
