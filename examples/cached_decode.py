@@ -39,11 +39,14 @@ class Model:
         """Last hidden states [B, N, HIDDEN] of `tokens` behind what sequences `seqs` have committed; their rows go into the cache."""
         B, N = tokens.shape
         x = self.embed[tokens.long()]
+        a = work = None                                  # (one of each for all layers: calls that are given both go through the binding's native part)
         for layer in range(LAYERS):
             rows = (x @ self.qkv[layer].T).view(B, N, HEADS + 2 * KV_HEADS, HEAD_DIM)
             q, k, v = rows.split((HEADS, KV_HEADS, KV_HEADS), 2)
             kv.mars_kv_append(c.pool, c.page_table, c.lens, k, v, layer=layer, seqs=seqs)
-            a, _ = kv.mars_kv_attention(c.pool, c.page_table, c.lens, q, layer=layer, seqs=seqs, mask=mask)
+            if work is None:
+                a, work = torch.empty(q.shape, dtype=q.dtype, device=q.device), kv.alloc_attention_workspace(c.pool, c.page_table, q)
+            kv.mars_kv_attention(c.pool, c.page_table, c.lens, q, layer=layer, seqs=seqs, mask=mask, out=a, workspace=work)
             x = x + a.reshape(B, N, -1) @ self.out[layer].T
             x = x * torch.rsqrt(x.float().square().mean(-1, keepdim=True)).bfloat16()
         return x

@@ -119,8 +119,9 @@ int mars_tree_mask(const int32_t* tree_parent, const int32_t* n_new, int B, int 
  *              longer sequences are attended in full.
  *   workspace  256-byte aligned, >= mars_kv_attention_workspace_bytes(...); scratch, calls that share it must not overlap.
  * Scores, softmax statistics and sums are held in fp32.  For bf16 rows the probabilities are rounded to bf16 in front of the
- * product with the values (a relative error of at most 2^-8 per key, independent from key to key); for fp32 rows they and the queries go through the
- * matrix cores as three bf16 terms each.  Results are reproducible bit for bit.
+ * product with the values (a relative error of at most 2^-8 per key; equal ones are rounded the same way); for fp32 rows they and the queries go through the
+ * matrix cores as three bf16 terms each (a query beyond bf16's largest number, 3.39e38, makes its row NaN).  Scores are those of fp32: q.k beyond its range is
+ * infinite, whatever scale makes of it.  Results are reproducible bit for bit.
  * A sequence number outside the cache gives rows of zeros (without seqs: requests from `sequences` on); a page number outside it among a row's keys gives NaN.
  * Reads page_table, lens.
  */

@@ -74,9 +74,11 @@ struct AttnPlan {
   u32 groups;      // work-groups beside each other on the chip
   size_t bytes;    // of pieces
 };
-// Up to 32 rows of bf16 the waves divide the keys: 28 rows over 4 caches of 60 000 - 131 000 tokens take 106 us so, and 165 in blocks of 16.  Beyond, 32
-// rows each, by 8 waves where their blocks hold no more rows than those of 4 (208 rows over long caches: 410 us, by 4 waves 480; but 288 rows over 16
-// caches of 1 024 - 8 191: 175 and 169; 100 rows: 89 and 77).
+// Up to 32 rows of bf16 the waves divide the keys: 28 rows over 4 caches of 60 000 - 131 000 tokens take 110 us so, and 165 in blocks of 16.  Beyond, 32
+// rows each, by 8 waves where their blocks hold no more rows than those of 4 (208 rows over long caches: 410 us, by 4 waves 480; 240 rows over 16 caches of 1 024 -
+// 8 191: 117 and 125; a prompt of 2 048 nodes, 64 blocks of four waves: 241 and 260), else by 4 (100 rows: 76 us, by 8 waves 90; 288 rows: 159 and 167; 352: 164 and 173;
+// 616, five blocks: 411 and 447).  With many blocks the odd one costs less than four waves do: 65 blocks, 2 049 or 2 080 nodes, take 272 us by 4 waves, and
+// would take 255 by 8; the rule leaves that.
 // In 32 bits the products take three times as long and 32 rows a third more registers: up to 80 rows 16 at a time are faster (48 rows: 47 us instead of 71, 80
 // rows: 66 and 77; 120 rows: 97 and 84).
 static AttnPlan attn_plan(int N, int group, int dim, int dtype, int page) {

@@ -7,7 +7,7 @@
 // byte permutation per two values.
 //
 // Few rows (Narrow, 16 or 32 at a time): the four waves of a work-group take every fourth tile of the same rows and meet in LDS at the end.  Bound by the cache's way from
-// memory: 64 tokens over 500 - 8 192, 304 MB, 69 us, of which in the middle 8.5 TB/s, the rest is the beginning and the end.
+// memory: 64 tokens over 500 - 8 192, 304 MB, 69 us, 4.4 TB/s, the way of the first tiles and the uneven ends included (64 channels, 152 MB: 43 us; 256, 304 MB: 71).
 // More (Wide): each of four or eight waves has 32 rows of its own, the values are converted once for all of them.  Bound by the matrix cores and the vector
 // instructions between them, and by the clock that the card keeps meanwhile.
 // The work is dealt out by kv_deal.h: a work-group takes a run of tiles that may begin and end inside a block of rows; what it has of such a
@@ -60,8 +60,11 @@ template <int TERMS> __device__ __forceinline__ void split_pair(float a, float b
 __device__ __forceinline__ u32 low_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
 __device__ __forceinline__ u32 high_halves(u32 a, u32 b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
-// The queries, as the first product's second operand, are bf16 rows as they are; fp32 rows are three bf16 terms, as the probabilities then are (one
-// term for bf16 rows, whose results are rounded to as many bits).  The matrix cores also take codes and scales as they are, by queries of 8 bits: two
+// The queries, as the first product's second operand, are bf16 rows as they are; fp32 rows are three bf16 terms, as the probabilities then are.  The
+// probabilities of bf16 rows are one term, which is a choice: results are 0.0023 from 64 bits, of which their own rounding is 0.0017.  A second term would
+// leave that alone, and cost 4 % with 64 tokens, 7 % with one, 15 % with 28 rows and 29 - 37 % where a wave has 32.  The sum l is that of the unrounded
+// ones, since lse is its logarithm; where all probabilities of a row are equal they are rounded the same way, and the row is off by up to that one rounding.
+// (Another sum, of the rounded ones, to divide by: 7 - 10 % with 32 rows per wave.)  The matrix cores also take codes and scales as they are, by queries of 8 bits: two
 // such terms hold a bf16 number, and the conversion of the keys falls away (a tenth of the time with long caches, nothing with few rows).  But
 // products of one instruction 2^16 below the largest are dropped there, and scores of 100 came out 1e-3 off; so it is not used.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -436,7 +439,9 @@ template <int D_, int RB, typename T_> struct Narrow {
 // step (64 keys for four waves, 128 for eight, of which one work-group fills a compute unit; two of four end 20% apart, as one is served first throughout).
 // 4 trees of 208 rows over 60 000 - 131 000 tokens: 410 us (0.83 PFLOP/s, 0.9 with the rows that fill up the last wave's 32; a large library product reaches
 // 1.2), by work-groups of four waves 480, by waves of 64 rows, one per SIMD, 580.  16 trees of 240 rows over 1 024 - 8 191: 107 us, by four 118.  The matrix
-// cores are busy for half of the clocks, of which there are 1.7 to 2.0 GHz under this load.  Scores a tile ahead, the exponentials laid between the matrix instructions,
+// cores are busy for 30 to 40 % of the clocks, of which there are 2.0 to 2.2 GHz under this load.  fp32 rows (four waves) take three times the products, and their terms of the
+// queries, 96 registers with 128 channels and 192 with 256, leave too few: 32 - 96 and 252 - 312 bytes of a lane are spilled.  16 trees of 240 rows over 1 024 - 8 191: 223 us
+// (bf16 111); four heads of 256 channels 445 (bf16 151).  Scores a tile ahead, the exponentials laid between the matrix instructions,
 // priorities and a deeper ring changed nothing or cost a little.
 template <int D> struct Keys32 {
   u32 k[D / 64][4], ks[D / 64];  // 32 channels each, 64 s + 32 h
@@ -690,7 +695,8 @@ template <typename W> struct Piece {
   __device__ __forceinline__ f32x4& part(int i, int lane) const { return reinterpret_cast<f32x4*>(at + 2 * W::kRows)[i * kWave + lane]; }
 };
 
-// Rows that see nothing because their request has fewer nodes (or no sequence): zeros.
+// Rows that see nothing because their request has fewer nodes (or no sequence): zeros, by one work-group per request in front of its share of the attention.  That is
+// what ragged prompts are bound by: 8 with 100 to 2 048 of N = 2 048 nodes behind up to 100 tokens 640 us, with 100 each 510, with all of them 450.
 template <typename T, int D> __device__ __forceinline__ void clear_rows(const AttnArgs& a, int b, int n) {
   const long items = static_cast<long>(a.N - n) * a.q_heads * (D / 8);
   for (long i = threadIdx.x; i < items; i += blockDim.x) {

@@ -70,7 +70,7 @@ template <int THREADS, typename F> __device__ void walk(const Cache& c, int B, c
 // a request has one such page at most, the one that its committed tokens end in, and they are compared in LDS; a sequence that was cut back to an
 // earlier token can have many, and then their writers are counted page by page in the workspace.
 // What bounds it: the latency of its chain of loads (sequence, length, page, count) and barriers, and the way through refs to the free
-// pages, 16 of them per thread and step.  A request's two children 7.5 us, 16 requests' eight each 13.
+// pages, 16 of them per thread and step.  A request's two children 8.6 us, 16 requests' eight each 13.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS) reserve_kernel(Cache c, const int32_t* __restrict__ seqs, const int32_t* __restrict__ n_new,
                                                                int B, int N, int32_t* __restrict__ status, ReserveSpace ws) {
@@ -351,8 +351,8 @@ __global__ void __launch_bounds__(256) release_kernel(Cache c, const int32_t* __
 
 // ---------------------------------------------------------------- the tree's mask
 // A work-group per request, a thread per node (up to four): it climbs to the root, its bits gathered word by word from the last on,
-// since an ancestor's number is smaller.  The parents lie in LDS; a tree is a few levels deep, a chain of N nodes N.  5 us, most of
-// it the launch.
+// since an ancestor's number is smaller.  The parents lie in LDS; a tree is a few levels deep, a chain of N nodes N.  Bound by the latency of that climb
+// (and of the launch, some 2 us): trees of 60 nodes 4.6 us, of 1 024 15; as chains 7 and 270 (a chain needs no mask).
 constexpr int kMaskThreads = 256;
 __global__ void __launch_bounds__(kMaskThreads) tree_mask_kernel(const int32_t* __restrict__ tree_parent, const int32_t* __restrict__ n_new,
                                                                  int N, unsigned long long* __restrict__ mask, int32_t* __restrict__ status) {

@@ -22,7 +22,8 @@ __device__ __forceinline__ void report(int32_t* status, int b, int value) {
 // An item is eight positions beside each other (an octet: the unit of the values' layout) of a head; D/8 lanes take eight channels
 // each and go through the octet's tokens, all of whose loads are under way before the first is used.  So a value's codes leave as
 // 32 contiguous bytes per lane where the whole octet is new, and no lane ever reads what another one writes.
-// 8 prompts of up to 8 192 tokens (8 heads of 128 channels, bf16, 254 MB read and written): 65 us, 3.9 TB/s, waiting for memory; 16 trees of 60 nodes 6.5 us.
+// 8 prompts of up to 8 192 tokens (8 heads of 128 channels): bf16, 198 MB read and written, 65 us, 3.0 TB/s, waiting for memory; fp32, 355 MB, 113 us, 3.1 TB/s (three waves per
+// SIMD instead of five).  16 trees of 60 nodes 6.2 us.  The status is found by one lane, page after page: 1 025 pages of 8 tokens 100 us, 129 of 64 tokens 5.
 template <int D, typename T>
 __global__ void __launch_bounds__(256) append_kernel(Cache c, size_t layer_offset, const int32_t* __restrict__ seqs, Rows<const T> k,
                                                      Rows<const T> v, const int32_t* __restrict__ n_new, int B, int N, int octets,
@@ -113,7 +114,8 @@ __device__ __forceinline__ void decode_eight(u32 codes, u32 byte, u32 (&w)[4]) {
   w[3] = decode<3>(codes, scale);
 }
 
-// The items of append, the other way round.  Positions without a page are zero.  The same prompts: 55 us, 4.6 TB/s, where a large copy reaches 4.9.
+// The items of append, the other way round.  Positions without a page are zero.  The same prompts, all N rows: bf16, 42 MB in and 268 out, 54 us, 5.7 TB/s, bound by
+// the way out (a large copy reaches 4.9 in both directions together); fp32, 579 MB, 143 us.
 template <int D, typename T>
 __global__ void __launch_bounds__(256) read_kernel(Cache c, size_t layer_offset, const int32_t* __restrict__ seqs,
                                                    const int32_t* __restrict__ first, Rows<T> k, Rows<T> v, int B, int N, int octets,
