@@ -40,13 +40,7 @@ def test_scores_near_the_least_number(dtype, N, group):
     assert ((lse.double() / (scale * -2.5 * 2.0 ** 126) - 1).abs() <= 2.0 ** -21).all()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("N,group", [(1, 4), (7, 4), (26, 4), (60, 4)])
-@pytest.mark.parametrize("size", [2.0 ** 12, 2.0 ** 25, 2.0 ** 33, 2.0 ** 64, 2.0 ** 120])
-def test_large_scores(size, N, group, dtype):
-    """Scores are exact (one channel), the largest of a row are equal: their values' mean is the result, however large they are."""
-    print("large", size, N, group, dtype, flush=True)
-    D, P, lens = 64, 16, (700, 40)
+def large_scores(size, N, group, dtype, D, P, lens):
     rng = np.random.default_rng(N)
     f = Filled(rng, lens, N, 1, D, P, rows=False)
     f.k, f.v = [], []
@@ -76,3 +70,20 @@ def test_large_scores(size, N, group, dtype):
             assert ((out[b, :, h].double() - want).abs() <= bound).all(), (b, h)
             want_lse = float(np.float32(scale)) * s.max() + math.log(top.sum())
             assert ((lse[b, :, h].double() - want_lse).abs() <= 2.0 ** -20 * abs(want_lse)).all(), (b, h)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,group", [(1, 4), (7, 4), (26, 4), (60, 4)])
+@pytest.mark.parametrize("size", [2.0 ** 12, 2.0 ** 25, 2.0 ** 33, 2.0 ** 64, 2.0 ** 120])
+def test_large_scores(size, N, group, dtype):
+    """Scores are exact (one channel), the largest of a row are equal: their values' mean is the result, however large they are."""
+    print("large", size, N, group, dtype, flush=True)
+    large_scores(size, N, group, dtype, 64, 16, (700, 40))
+
+
+@pytest.mark.parametrize("dtype,D,P,N", [("bf16", 128, 64, 1), ("bf16", 256, 32, 2), ("bf16", 128, 16, 7), ("bf16", 64, 64, 40), ("bf16", 128, 64, 60), ("f32", 128, 8, 3),
+                                         ("f32", 64, 64, 30)])
+def test_large_scores_of_pieces_that_are_joined(dtype, D, P, N):
+    print("large, joined", dtype, D, P, N, flush=True)
+    for size in (2.0 ** 12, 2.0 ** 40):
+        large_scores(size, N, 4, dtype, D, P, (2600, 1500))
